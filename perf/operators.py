@@ -370,7 +370,8 @@ def _own_run(state):
     case = state["case"]
     op, grid = case["op"], (case["T"], case["H"], case["W"])
     if op in ("norm_rope", "norm_rope_bwd"):
-        how = dict(dims=DIMS[case["dims"]], theta=THETA, norm=case["norm"], q_weight=state["q_weight"], k_weight=state["k_weight"], eps=EPS,
+        weights = ("q_weight", "k_weight") if case["norm"] != "none" else ()   # (rotation alone has none)
+        how = dict(dims=DIMS[case["dims"]], theta=THETA, norm=case["norm"], **{w: state[w] for w in weights}, eps=EPS,
                    pairs=case["pairs"], origin=(case["origin"],) * 3, step=(case["step"],) * 3, n_text=case["text"], first_token=case["first"])
         if op == "norm_rope":
             return psa.psa_qk_norm_rope(state["q"], state["k"], grid, **how)
