@@ -204,6 +204,59 @@ int psa_search_losses(const void* q, const void* k, const void* v, const psa_hea
 int psa_search_select(const float* losses, const float* sparsity, int n, float alpha);
 int psa_search_select_at_sparsity(const float* losses, const float* sparsity, int n, float target);
 
+/* What a layer does to its queries and keys before attention: root-mean-square norm and rotary positions on the frame, row
+ * and column axes, in one pass.  (The paper takes q and k as the model's blocks hand them over.)  For x of one token and
+ * head, 128 channels:
+ *   r = 1 / sqrt(mean(x^2) + eps)   the mean over the head's channels (PSA_NORM_HEAD), or over the channels of all heads of the
+ *                                   token (PSA_NORM_TOKEN); PSA_NORM_NONE: r = 1 and no weights
+ *   u = x * r * weight              weight: [128], or [n_heads][128]; NULL: 1
+ *   the first dim_t / 2 pairs of channels turn with the token's frame, the next dim_h / 2 with its row, the next dim_w / 2 with
+ *   its column, channels beyond dim_t + dim_h + dim_w = R not at all.  Pair j of an axis of d channels turns by
+ *   (origin + step * index) * theta^(-2 j / d), computed in 64 bits.  Pair p is channels 2p and 2p + 1, or p and p + R / 2
+ *   (PSA_PAIRS_HALVES; R a multiple of 8):  (a, b) -> (a cos - b sin, a sin + b cos).
+ * Tokens T*H*W .. T*H*W + n_text - 1 of the sequence (text) are normed and not rotated.  The tensors hold tokens first_token ..
+ * first_token + n_tokens - 1 of the sequence, e.g. one rank's part (n_tokens 0: nothing happens).  Arithmetic in 32 bits, one
+ * rounding at the end.
+ *   q, k             device, element (b, head, token, c) at b*stride_batch + head*stride_head + token*stride_token + c, of dtype;
+ *                    k may be NULL (with its output, weight and gradients)
+ *   q_out, k_out     the same with out_stride_*, of out_dtype: dtype, or PSA_BF16 from the others.  They may be q and k
+ *                    themselves if types and strides agree, and must not overlap them otherwise
+ *   q_weight, k_weight   device, contiguous, of weight_dtype
+ * Pointers (but for those of dq_weight, dk_weight, 4 bytes) must be 16-byte aligned, strides multiples of 8.  n_heads <= 128.
+ *
+ * psa_qk_norm_rope_bwd: from the gradients dq_out, dk_out of the outputs (out_dtype, out_stride_*) those of q and k (dtype,
+ * grad_stride_*; must not overlap anything else) and of the weights (device fp32 [weight_heads][128], sums over all tokens;
+ * both or neither NULL, and NULL for PSA_NORM_NONE).  q and k are the forward call's (for PSA_NORM_NONE not read, may be NULL).
+ * scratch: device, 16-byte aligned, psa_qk_norm_rope_bwd_scratch_bytes(prob) bytes, needed with weight gradients only.  Sums run
+ * in a fixed order: a call repeated gives the same bits. */
+typedef enum { PSA_BF16 = 0, PSA_FP16 = 1, PSA_FP32 = 2 } psa_dtype;
+typedef enum { PSA_NORM_NONE = 0, PSA_NORM_HEAD = 1, PSA_NORM_TOKEN = 2 } psa_norm;
+typedef enum { PSA_PAIRS_INTERLEAVED = 0, PSA_PAIRS_HALVES = 1 } psa_pairs;
+typedef struct {
+  int32_t n_batch, n_heads, head_dim;   /* head_dim must be 128 */
+  int32_t dtype, out_dtype;             /* psa_dtype            */
+  int32_t norm;                         /* psa_norm             */
+  int32_t weight_dtype, weight_heads;   /* weight_heads: 1 or n_heads */
+  float   eps;                          /* >= 0                 */
+  int32_t reserved;                     /* 0                    */
+  int64_t n_tokens, first_token, n_text;
+  int64_t stride_batch, stride_head, stride_token;
+  int64_t out_stride_batch, out_stride_head, out_stride_token;
+  int64_t grad_stride_batch, grad_stride_head, grad_stride_token;
+} psa_qk;
+typedef struct {
+  int32_t dim_t, dim_h, dim_w;          /* even, >= 0, sum <= 128 */
+  int32_t pairs;                        /* psa_pairs              */
+  double  theta;                        /* > 0                    */
+  double  origin[3], step[3];           /* frame, row, column     */
+} psa_rope;
+int psa_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, const void* q_weight, const void* k_weight,
+                     const psa_qk* prob, const psa_rope* rope, int T, int H, int W, void* stream);
+int64_t psa_qk_norm_rope_bwd_scratch_bytes(const psa_qk* prob);
+int psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, void* dq, void* dk,
+                         const void* q_weight, const void* k_weight, float* dq_weight, float* dk_weight,
+                         const psa_qk* prob, const psa_rope* rope, int T, int H, int W, void* scratch, void* stream);
+
 /* Synchronises the current device, then returns the status word the last psa_attn_fwd
  * on it left behind: PSA_OK, or PSA_ERR_TIMEOUT if a bounded wait inside the kernel
  * expired (outputs are then undefined); also what a replay of a call captured in a CUDA graph

@@ -77,6 +77,12 @@ def lib() -> ctypes.CDLL:
         L.psa_search_select.restype = ctypes.c_int
         L.psa_search_select_at_sparsity.argtypes = L.psa_search_select.argtypes
         L.psa_search_select_at_sparsity.restype = ctypes.c_int
+        L.psa_qk_norm_rope.argtypes = [vp] * 8 + [i32, i32, i32, vp]
+        L.psa_qk_norm_rope.restype = ctypes.c_int
+        L.psa_qk_norm_rope_bwd_scratch_bytes.argtypes = [vp]
+        L.psa_qk_norm_rope_bwd_scratch_bytes.restype = ctypes.c_int64
+        L.psa_qk_norm_rope_bwd.argtypes = [vp] * 12 + [i32, i32, i32, vp, vp]
+        L.psa_qk_norm_rope_bwd.restype = ctypes.c_int
         L.psa_last_device_status.argtypes = [ctypes.POINTER(ctypes.c_int32)]
         L.psa_last_attn_launch.argtypes = [ctypes.POINTER(ctypes.c_int32)] * 2
         L.psa_last_attn_launch.restype = ctypes.c_int
@@ -394,6 +400,152 @@ def psa_search_select_at_sparsity(losses: Sequence[float], sparsity: Sequence[fl
     if r < 0:
         _check(r, "psa_search_select_at_sparsity")
     return r
+
+
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    """Device tensors of the current device (kernels are launched there)."""
+    here = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("device tensors required")
+        if here is None:
+            here = torch._C._cuda_getDevice()
+        if t.device.index != here:
+            raise ValueError("tensors must be on the current device")
+
+
+def _used_on(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> None:
+    """Memory allocated here on the current stream and used on `stream`."""
+    if stream is not None and stream != torch.cuda.current_stream():
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_NORMS = {"none": 0, "head": 1, "token": 2}
+_PAIRS = {"interleaved": 0, "halves": 1}
+_pack_qk = struct.Struct("8ifi12q").pack     # the layout of psa_qk
+_pack_rope = struct.Struct("4i7d").pack      # the layout of psa_rope
+
+
+def _strides4(t: torch.Tensor) -> Tuple[int, int, int]:
+    """Strides of batch, head and token of [(batch,) heads, tokens, channels]; the channels must be contiguous."""
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError("a contiguous last dimension is required")
+    return (0, st[0], st[1]) if len(st) == 3 else st[:3]
+
+
+def _norm_rope_call(first: torch.Tensor, out: torch.Tensor, grad: Optional[torch.Tensor], dtype: torch.dtype, q_weight, k_weight, two: bool,
+                    dims, theta, norm, eps, pairs, origin, step, n_text, first_token) -> Tuple[bytes, bytes, int]:
+    """psa_qk and psa_rope of a call as packed bytes, and the heads that the weights are of (0: no weights)."""
+    shape = first.shape
+    if len(shape) not in (3, 4):
+        raise ValueError("[heads, tokens, channels] or [batch, heads, tokens, channels] required")
+    batch, heads, tokens, d = shape if len(shape) == 4 else (1, *shape)
+    if norm not in _NORMS or pairs not in _PAIRS:
+        raise ValueError("norm is one of %s, pairs one of %s" % (", ".join(_NORMS), ", ".join(_PAIRS)))
+    if dtype not in _DTYPES or out.dtype not in _DTYPES:
+        raise ValueError("bf16, fp16 or fp32 tensors required")
+    weight_heads, weight_dtype = 0, torch.float32
+    for w in (q_weight, k_weight):
+        if w is None:
+            continue
+        if tuple(w.shape) not in ((d,), (heads, d)) or not w.is_contiguous() or w.dtype not in _DTYPES:
+            raise ValueError("weights are contiguous [channels] or [heads, channels] tensors of bf16, fp16 or fp32")
+        n = 1 if w.dim() == 1 else heads
+        if weight_heads and (n, w.dtype) != (weight_heads, weight_dtype):
+            raise ValueError("both weights must be alike")
+        weight_heads, weight_dtype = n, w.dtype
+    if norm == "none" and weight_heads:
+        raise ValueError("there are no weights without a norm")
+    if two and norm != "none" and (q_weight is None) != (k_weight is None):
+        raise ValueError("weights for both tensors or for none")
+    if not two and k_weight is not None:
+        raise ValueError("a weight for k without k")
+    prob = _pack_qk(batch, heads, d, _DTYPES[dtype], _DTYPES[out.dtype], _NORMS[norm], _DTYPES[weight_dtype], max(weight_heads, 1), eps, 0, tokens,
+                    int(first_token), int(n_text), *_strides4(first), *_strides4(out), *(_strides4(grad) if grad is not None else (0, 0, 0)))
+    dt, dh, dw = dims
+    rope = _pack_rope(int(dt), int(dh), int(dw), _PAIRS[pairs], theta, *origin, *step)
+    return prob, rope, weight_heads
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def psa_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], grid: Sequence[int], dims: Sequence[int] = (44, 42, 42), theta: float = 10000.0,
+                     norm: str = "head", q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     pairs: str = "interleaved", origin: Sequence[float] = (0.0, 0.0, 0.0), step: Sequence[float] = (1.0, 1.0, 1.0),
+                     n_text: int = 0, first_token: int = 0, out: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                     out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Root-mean-square norm and rotary positions of queries and keys (see psa.h), in one pass.
+
+    q, k: bf16, fp16 or fp32 device tensors [heads, tokens, 128] or [batch, heads, tokens, 128] sharing shape, strides and type (the
+    last dimension contiguous; views of a fused projection will do); k may be None.  They hold tokens ``first_token`` .. of the sequence
+    of T*H*W video tokens and ``n_text`` text tokens, which are normed and not rotated.
+    ``dims``: channels that turn with the frame, the row and the column.  ``norm``: "head", "token" (over all heads) or "none"; weights
+    [128] or [heads, 128].  Positions are ``origin + step * index``.  ``out``: (q_out, k_out), which may be (q, k); by default new
+    tensors of q's layout without gaps, of ``out_dtype`` (q's type, or bf16).  Returns (q_out, k_out)."""
+    two = k is not None
+    if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
+        raise ValueError("q and k must share shape, strides and type")
+    if out is None:
+        q_out = torch.empty_like(q, dtype=out_dtype)
+        k_out = torch.empty_like(k, dtype=out_dtype) if two else None
+        _used_on(stream, q_out, k_out)
+    else:
+        q_out, k_out = out
+        if q_out.shape != q.shape or (k_out is not None) != two or (out_dtype is not None and q_out.dtype != out_dtype):
+            raise ValueError("out must be (q_out, k_out) of q's shape")
+    if two and (k_out.shape != q_out.shape or k_out.stride() != q_out.stride() or k_out.dtype != q_out.dtype):
+        raise ValueError("q_out and k_out must share shape, strides and type")
+    _on_current_device(q, k, q_out, k_out, q_weight, k_weight)
+    prob, rope, _ = _norm_rope_call(q, q_out, None, q.dtype, q_weight, k_weight, two, dims, theta, norm, eps, pairs, origin, step, n_text, first_token)
+    T, H, W = map(int, grid)
+    _check(lib().psa_qk_norm_rope(q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), _ptr(q_weight), _ptr(k_weight), prob, rope, T, H, W,
+                                  _stream_ptr(stream)), "psa_qk_norm_rope")
+    return q_out, k_out
+
+
+def psa_qk_norm_rope_bwd(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                         grid: Sequence[int], dims: Sequence[int] = (44, 42, 42), theta: float = 10000.0, norm: str = "head",
+                         q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                         pairs: str = "interleaved", origin: Sequence[float] = (0.0, 0.0, 0.0), step: Sequence[float] = (1.0, 1.0, 1.0),
+                         n_text: int = 0, first_token: int = 0, stream: Optional[torch.cuda.Stream] = None):
+    """Gradient of psa_qk_norm_rope: from the gradients of its outputs (sharing shape, strides and type) and its inputs, which norm
+    "none" does not need (None).  Returns (dq, dk, dq_weight, dk_weight): of q's type and layout without gaps, and fp32; None for
+    what there is no input for."""
+    two = dk_out is not None
+    if two and (dk_out.shape != dq_out.shape or dk_out.stride() != dq_out.stride() or dk_out.dtype != dq_out.dtype):
+        raise ValueError("dq_out and dk_out must share shape, strides and type")
+    if q is None and (k is not None or norm != "none"):
+        raise ValueError("q and k are needed with a norm")
+    like = dq_out if q is None else q
+    if q is not None:
+        if q.shape != dq_out.shape or (k is not None) != two:
+            raise ValueError("q and k must be those of the outputs")
+        if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
+            raise ValueError("q and k must share shape, strides and type")
+    dq = torch.empty_like(like)
+    dk = torch.empty_like(like) if two else None
+    _on_current_device(dq_out, dk_out, q, k, q_weight, k_weight)
+    prob, rope, weight_heads = _norm_rope_call(like, dq_out, dq, like.dtype, q_weight, k_weight, two, dims, theta, norm, eps, pairs, origin, step,
+                                               n_text, first_token)
+    dq_weight = dk_weight = scratch = None
+    if weight_heads:
+        dq_weight = torch.empty(q_weight.shape, dtype=torch.float32, device=q.device)
+        dk_weight = torch.empty_like(dq_weight) if two else None
+        scratch = torch.empty(int(lib().psa_qk_norm_rope_bwd_scratch_bytes(prob)), dtype=torch.uint8, device=q.device)
+    _used_on(stream, dq, dk, dq_weight, dk_weight, scratch)
+    T, H, W = map(int, grid)
+    _check(lib().psa_qk_norm_rope_bwd(dq_out.data_ptr(), _ptr(dk_out), _ptr(q), _ptr(k), dq.data_ptr(), _ptr(dk), _ptr(q_weight), _ptr(k_weight),
+                                      _ptr(dq_weight), _ptr(dk_weight), prob, rope, T, H, W, _ptr(scratch), _stream_ptr(stream)),
+           "psa_qk_norm_rope_bwd")
+    return dq, dk, dq_weight, dk_weight
 
 
 LAUNCH_MODES = ("ticket", "direct", "shared", "shared_direct", "ticket_edge", "ticket_short")

@@ -15,8 +15,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpsa.so")
 LIB_CHECKED = os.path.join(HERE, "libpsa_checked.so")
-SOURCES = ["psa_host.cu", "psa_mask_build.cu", "psa_attn_sm100.cu", "psa_search.cu"]
-HEADERS = [os.path.join(CSRC, "psa_common.cuh"), os.path.join(ROOT, "include", "psa.h")]
+SOURCES = ["psa_host.cu", "psa_mask_build.cu", "psa_attn_sm100.cu", "psa_search.cu", "psa_norm_rope.cu"]
+HEADERS = [os.path.join(CSRC, "psa_common.cuh"), os.path.join(CSRC, "psa_norm_rope.cuh"), os.path.join(ROOT, "include", "psa.h")]
 
 
 def _nvcc():
@@ -39,7 +39,7 @@ def build(force=False, verbose=False, checked=False):
     if not force and not needs_build(lib):
         return lib
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+           "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-o", lib] + (["-DPSA_DEBUG_CHECKS"] if checked else []) + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas")

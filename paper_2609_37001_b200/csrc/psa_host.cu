@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "psa_common.cuh"
+#include "psa_norm_rope.cuh"
 
 namespace psa {
 bool mask_build_small(const Geom& g);
@@ -1307,6 +1308,140 @@ int psa_attn_fwd_host(const void* q, const void* k, const void* v, void* out, fl
   if (cudaStreamWaitEvent(st, pipe->ev_end, 0) != cudaSuccess) return PSA_ERR_CUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return PSA_ERR_CUDA;
   return PSA_OK;
+}
+
+// Checks what psa_qk_norm_rope and its gradient have in common and fills the kernels' arguments but for the pointers.
+// *nothing: there are no tokens.
+static int norm_rope_args(const psa_qk* prob, const psa_rope* rope, int T, int H, int W, NormRopeArgs* a, bool* nothing) {
+  if (!prob || !rope || T < 1 || H < 1 || W < 1 || prob->n_batch < 1 || prob->n_heads < 1) return PSA_ERR_INVALID_ARG;
+  if (prob->head_dim != kHeadDim || prob->n_heads > kMaxHeads) return PSA_ERR_UNSUPPORTED;
+  const long long L = (long long)T * H * W, lim = 1ll << 31;
+  if ((long long)T * H >= lim || L >= lim) return PSA_ERR_INVALID_ARG;
+  if (prob->n_text < 0 || prob->n_text >= lim || prob->first_token < 0 || prob->n_tokens < 0 || prob->n_tokens >= lim ||
+      prob->first_token >= lim * 2 || prob->first_token + prob->n_tokens > L + prob->n_text)
+    return PSA_ERR_INVALID_ARG;
+  if (prob->n_tokens * (long long)prob->n_batch >= lim) return PSA_ERR_UNSUPPORTED;
+  if (prob->dtype < PSA_BF16 || prob->dtype > PSA_FP32 || prob->out_dtype < PSA_BF16 || prob->out_dtype > PSA_FP32) return PSA_ERR_INVALID_ARG;
+  if (prob->out_dtype != prob->dtype && prob->out_dtype != PSA_BF16) return PSA_ERR_UNSUPPORTED;
+  if (prob->norm < PSA_NORM_NONE || prob->norm > PSA_NORM_TOKEN || prob->weight_dtype < PSA_BF16 || prob->weight_dtype > PSA_FP32) return PSA_ERR_INVALID_ARG;
+  if (prob->weight_heads != 1 && prob->weight_heads != prob->n_heads) return PSA_ERR_INVALID_ARG;
+  if (!(prob->eps >= 0.f) || !std::isfinite(prob->eps)) return PSA_ERR_INVALID_ARG;
+  const int dims[3] = {rope->dim_t, rope->dim_h, rope->dim_w};
+  for (int d : dims)
+    if (d < 0 || d > kHeadDim || (d & 1)) return PSA_ERR_INVALID_ARG;
+  const int rotated = dims[0] + dims[1] + dims[2];
+  if (rotated > kHeadDim || (rope->pairs != PSA_PAIRS_INTERLEAVED && rope->pairs != PSA_PAIRS_HALVES)) return PSA_ERR_INVALID_ARG;
+  if (rope->pairs == PSA_PAIRS_HALVES && rotated % 8 != 0) return PSA_ERR_UNSUPPORTED;
+  if (!(rope->theta > 0.0) || !std::isfinite(rope->theta)) return PSA_ERR_INVALID_ARG;
+  std::memset(a, 0, sizeof(*a));
+  for (int x = 0, p = 0; x < 3; ++x) {
+    if (!std::isfinite(rope->origin[x]) || !std::isfinite(rope->step[x])) return PSA_ERR_INVALID_ARG;
+    a->origin[x] = rope->origin[x];
+    a->step[x] = rope->step[x];
+    for (int j = 0; j < dims[x] / 2; ++j) a->turns[p++] = std::pow(rope->theta, -2.0 * j / dims[x]) / 6.283185307179586476925;
+    a->pairs[x] = p;
+  }
+  a->H = H;
+  a->W = W;
+  a->n_video = L;
+  a->first_token = prob->first_token;
+  a->n_tokens = (int)prob->n_tokens;
+  a->n_all = (int)(prob->n_tokens * prob->n_batch);
+  a->n_heads = prob->n_heads;
+  a->weight_dtype = prob->weight_dtype;
+  a->weight_head = prob->weight_heads != 1;
+  a->weight_cols = prob->weight_heads * kHeadDim;
+  a->eps = prob->eps;
+  a->inv_count = 1.f / (float)(kHeadDim * (prob->norm == PSA_NORM_TOKEN ? prob->n_heads : 1));
+  *nothing = prob->n_tokens == 0;
+  return PSA_OK;
+}
+// Strides of a tensor with more than one element along the axis.
+static bool valid_strides(const psa_qk* p, int64_t batch, int64_t head, int64_t token) {
+  auto ok = [](int64_t n, int64_t s) { return n <= 1 || (s >= kHeadDim && s % 8 == 0); };
+  return ok(p->n_batch, batch) && ok(p->n_heads, head) && ok(p->n_tokens, token);
+}
+
+int psa_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, const void* q_weight, const void* k_weight, const psa_qk* prob,
+                     const psa_rope* rope, int T, int H, int W, void* stream) {
+  NormRopeArgs a;
+  bool nothing;
+  const int rc = norm_rope_args(prob, rope, T, H, W, &a, &nothing);
+  if (rc != PSA_OK) return rc;
+  if (nothing) return PSA_OK;
+  if (!q || !q_out || (k == nullptr) != (k_out == nullptr) || (!k && k_weight)) return PSA_ERR_INVALID_ARG;
+  if (prob->norm == PSA_NORM_NONE && (q_weight || k_weight)) return PSA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight)) return PSA_ERR_INVALID_ARG;
+  if (!valid_strides(prob, prob->stride_batch, prob->stride_head, prob->stride_token) ||
+      !valid_strides(prob, prob->out_stride_batch, prob->out_stride_head, prob->out_stride_token))
+    return PSA_ERR_INVALID_ARG;
+  const bool alike = prob->dtype == prob->out_dtype && (prob->n_batch == 1 || prob->stride_batch == prob->out_stride_batch) &&
+                     (prob->n_heads == 1 || prob->stride_head == prob->out_stride_head) && (prob->n_tokens == 1 || prob->stride_token == prob->out_stride_token);
+  if (!alike && (q == q_out || (k && k == k_out))) return PSA_ERR_INVALID_ARG;
+  a.in[0] = q; a.in[1] = k;
+  a.out[0] = q_out; a.out[1] = k_out;
+  a.weight[0] = q_weight; a.weight[1] = k_weight;
+  a.in_batch = prob->stride_batch; a.in_head = prob->stride_head; a.in_token = prob->stride_token;
+  a.out_batch = prob->out_stride_batch; a.out_head = prob->out_stride_head; a.out_token = prob->out_stride_token;
+  std::lock_guard<std::mutex> lock(g_mu);
+  int dev, launches = 0;
+  Workspace* ws;
+  if (const int rc2 = device_info(&dev, &ws)) return rc2;
+  const cudaError_t e = launch_norm_rope(a, *prob, rope->pairs == PSA_PAIRS_HALVES, false, ws->n_sms, nullptr, nullptr, static_cast<cudaStream_t>(stream), &launches);
+  g_launches += launches;
+  return e == cudaSuccess ? PSA_OK : PSA_ERR_CUDA;
+}
+
+int64_t psa_qk_norm_rope_bwd_scratch_bytes(const psa_qk* prob) {
+  if (!prob || prob->weight_heads < 1) return PSA_ERR_INVALID_ARG;
+  if (prob->weight_heads > kMaxHeads) return PSA_ERR_UNSUPPORTED;
+  return 2ll * kNormRopeBwdBlocks * prob->weight_heads * kHeadDim * (long long)sizeof(float);
+}
+
+int psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, const void* k, void* dq, void* dk, const void* q_weight,
+                         const void* k_weight, float* dq_weight, float* dk_weight, const psa_qk* prob, const psa_rope* rope, int T, int H, int W,
+                         void* scratch, void* stream) {
+  NormRopeArgs a;
+  bool nothing;
+  const int rc = norm_rope_args(prob, rope, T, H, W, &a, &nothing);
+  if (rc != PSA_OK) return rc;
+  const bool norm = prob->norm != PSA_NORM_NONE, two = dk_out != nullptr || dk != nullptr;
+  if (!norm && (q_weight || k_weight || dq_weight || dk_weight)) return PSA_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (nothing) {   // sums over no tokens (whose tensors may have no address)
+    for (float* w : {dq_weight, dk_weight})
+      if (w && cudaMemsetAsync(w, 0, sizeof(float) * (size_t)a.weight_cols, st) != cudaSuccess) return PSA_ERR_CUDA;
+    return PSA_OK;
+  }
+  if ((!two && (k_weight || dk_weight)) || (dk_weight != nullptr) != (two && dq_weight != nullptr)) return PSA_ERR_INVALID_ARG;
+  if (!dq_out || !dq || (two && (!dk_out || !dk)) || (norm && (!q || (two && !k)))) return PSA_ERR_INVALID_ARG;
+  if (dq_weight && !scratch) return PSA_ERR_INVALID_ARG;
+  for (const void* p : {dq_out, dk_out, q, k, (const void*)dq, (const void*)dk, q_weight, k_weight, (const void*)scratch})
+    if (!aligned16(p)) return PSA_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(dq_weight) & 3u) || (reinterpret_cast<uintptr_t>(dk_weight) & 3u)) return PSA_ERR_INVALID_ARG;
+  if ((norm && !valid_strides(prob, prob->stride_batch, prob->stride_head, prob->stride_token)) ||
+      !valid_strides(prob, prob->out_stride_batch, prob->out_stride_head, prob->out_stride_token) ||
+      !valid_strides(prob, prob->grad_stride_batch, prob->grad_stride_head, prob->grad_stride_token))
+    return PSA_ERR_INVALID_ARG;
+  for (const void* to : {dq, dk})
+    for (const void* from : {dq_out, dk_out, q, k})
+      if (to && to == from) return PSA_ERR_INVALID_ARG;
+  if (dq == dk) return PSA_ERR_INVALID_ARG;
+  a.in[0] = norm ? q : nullptr; a.in[1] = norm && two ? k : nullptr;
+  a.grad[0] = dq_out; a.grad[1] = two ? dk_out : nullptr;
+  a.out[0] = dq; a.out[1] = dk;
+  a.weight[0] = q_weight; a.weight[1] = k_weight;
+  a.dw_part = dq_weight ? static_cast<float*>(scratch) : nullptr;
+  a.in_batch = prob->stride_batch; a.in_head = prob->stride_head; a.in_token = prob->stride_token;
+  a.out_batch = prob->out_stride_batch; a.out_head = prob->out_stride_head; a.out_token = prob->out_stride_token;
+  a.dx_batch = prob->grad_stride_batch; a.dx_head = prob->grad_stride_head; a.dx_token = prob->grad_stride_token;
+  std::lock_guard<std::mutex> lock(g_mu);
+  int dev, launches = 0;
+  Workspace* ws;
+  if (const int rc2 = device_info(&dev, &ws)) return rc2;
+  const cudaError_t e = launch_norm_rope(a, *prob, rope->pairs == PSA_PAIRS_HALVES, true, ws->n_sms, dq_weight, dk_weight, st, &launches);
+  g_launches += launches;
+  return e == cudaSuccess ? PSA_OK : PSA_ERR_CUDA;
 }
 
 int psa_selftest_wait_timeout(int limit_ms, void* stream) {
