@@ -178,6 +178,40 @@ int psa_attn_fwd_joint(const void* q, const void* k, const void* v, void* out, f
                        const psa_head_params* head_params, const psa_problem* prob, int64_t n_text,
                        int T, int H, int W, void* stream);
 
+/* Chooses key blocks for every query block by a score that pools the blocks (the paper's masks do not depend on the data; this is
+ * for heads whose attention no stripes describe):  with Q_i and K_j the sums of q and k over the tokens of blocks i and j, and n_j the
+ * tokens of block j,  s_ij = (Q_i . K_j) / n_j,  and block i of head h keeps the keep[h] blocks with the largest s_ij, equal ones
+ * by the lowest block, NaN as -infinity; with keep_self != 0 block i itself is always among them.  Sums and scores are in 64 bits.
+ *   q, k       device bf16, as psa_attn_fwd takes them (the T*H*W video tokens; prob->scale is not used)
+ *   keep       host, n_heads entries, 1 .. NB
+ *   row_ptr    device int32 [n_heads*NB + 1], col_idx device int32 [col_capacity]: the lists in the order and form of psa_mask_build,
+ *              sum of keep[h] * NB entries (PSA_ERR_CAPACITY if there are more than col_capacity)
+ *   scratch    device, 16-byte aligned, psa_select_scratch_bytes(...) bytes; calls that may overlap on the GPU need one each
+ * Any tile; the block grid has at most 3,500 blocks (what 227 KB of shared memory hold of 8 rows of scores).  Asynchronous on `stream`;
+ * allocates nothing. */
+int64_t psa_select_scratch_bytes(const psa_problem* prob, int T, int H, int W);
+int psa_select_blocks(const void* q, const void* k, const psa_problem* prob, int T, int H, int W, const int32_t* keep, int keep_self,
+                      int32_t* row_ptr, int32_t* col_idx, int64_t col_capacity, void* scratch, void* stream);
+
+/* Attention over lists of key blocks: psa_attn_fwd_joint with the mask given block by block instead of by stripes -- what
+ * psa_select_blocks or psa_mask_build wrote, or any other lists of the caller's (a mask that depends on the data has no six
+ * integers).  The paper's masks are stripes; lists in this form are those of psa_mask_build.
+ *   row_ptr   device int32 [n_heads*NB + 1]: query block i of head h attends key blocks col_idx[row_ptr[r]] ..
+ *             col_idx[row_ptr[r + 1] - 1], r = h*NB + i, ascending; none: out = 0 and lse = -inf for its tokens (with text:
+ *             the text alone)
+ *   col_idx   device int32 [n_entries] (may be NULL if n_entries is 0)
+ *   n_text    as for psa_attn_fwd_joint: text keys are attended by every query, text queries attend every key
+ *   scratch   device, 16-byte aligned, psa_attn_fwd_lists_scratch_bytes(...) bytes; calls that may overlap on the GPU, and graphs
+ *             that may, need one each
+ * Lists are read by the kernels only: a row that does not lie within the n_entries entries, or has more than NB, counts as
+ * empty, an entry that is no block or does not come behind the one before it is left out, and psa_last_device_status() reports
+ * PSA_ERR_INVALID_ARG (detail 0x600 or 0x601); out and lse of other rows are not affected.  What an entry's block holds beyond the
+ * grid is not attended.  Allocates nothing.  Everything else as psa_attn_fwd. */
+int64_t psa_attn_fwd_lists_scratch_bytes(const psa_problem* prob, int64_t n_text, int T, int H, int W);
+int psa_attn_fwd_lists(const void* q, const void* k, const void* v, void* out, float* lse, const int32_t* row_ptr,
+                       const int32_t* col_idx, int64_t n_entries, const psa_problem* prob, int64_t n_text,
+                       int T, int H, int W, void* scratch, void* stream);
+
 /* PSA-Search for ONE head (Appendix C, Algorithm 3).
  *
  * psa_search_losses: the inner loop -- Loss(M) = L2Loss(PSA(h, M), FullAttn(h)) for every candidate

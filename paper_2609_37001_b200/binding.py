@@ -77,6 +77,14 @@ def lib() -> ctypes.CDLL:
         L.psa_search_select.restype = ctypes.c_int
         L.psa_search_select_at_sparsity.argtypes = L.psa_search_select.argtypes
         L.psa_search_select_at_sparsity.restype = ctypes.c_int
+        L.psa_select_scratch_bytes.argtypes = [vp, i32, i32, i32]
+        L.psa_select_scratch_bytes.restype = ctypes.c_int64
+        L.psa_select_blocks.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, ctypes.c_int64, vp, vp]
+        L.psa_select_blocks.restype = ctypes.c_int
+        L.psa_attn_fwd_lists_scratch_bytes.argtypes = [vp, ctypes.c_int64, i32, i32, i32]
+        L.psa_attn_fwd_lists_scratch_bytes.restype = ctypes.c_int64
+        L.psa_attn_fwd_lists.argtypes = [vp] * 7 + [ctypes.c_int64, vp, ctypes.c_int64, i32, i32, i32, vp, vp]
+        L.psa_attn_fwd_lists.restype = ctypes.c_int
         L.psa_qk_norm_rope.argtypes = [vp] * 8 + [i32, i32, i32, vp]
         L.psa_qk_norm_rope.restype = ctypes.c_int
         L.psa_qk_norm_rope_bwd_scratch_bytes.argtypes = [vp]
@@ -546,6 +554,110 @@ def psa_qk_norm_rope_bwd(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q
                                       _ptr(dq_weight), _ptr(dk_weight), prob, rope, T, H, W, _ptr(scratch), _stream_ptr(stream)),
            "psa_qk_norm_rope_bwd")
     return dq, dk, dq_weight, dk_weight
+
+
+def psa_select_scratch_bytes(n_heads: int, grid: Sequence[int], tile: Sequence[int]) -> int:
+    """Bytes of device scratch that psa_select_blocks needs."""
+    T, H, W = map(int, grid)
+    n = int(lib().psa_select_scratch_bytes(_problem(n_heads, tile, 1.0, 0, 128), T, H, W))
+    if n < 0:
+        _check(n, "psa_select_scratch_bytes")
+    return n
+
+
+def psa_select_blocks(q: torch.Tensor, k: torch.Tensor, grid: Sequence[int], tile: Sequence[int], keep, keep_self: bool = False,
+                      out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, scratch: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Key blocks with the largest pooled scores for every query block (see psa.h): q, k are bf16 device tensors [heads, T*H*W, 128]
+    sharing strides (of a joint sequence: its video tokens, q[:, :T*H*W]), ``keep`` the number of blocks, one for all heads or one
+    each.  Returns (row_ptr int32 [heads * blocks + 1], col_idx int32), in ``out`` if given; ``scratch`` (uint8,
+    psa_select_scratch_bytes long) is allocated when not given."""
+    nh, L, d = q.shape
+    T, H, W = map(int, grid)
+    if L != T * H * W or k.shape != q.shape:
+        raise ValueError("shape mismatch")
+    _on_current_device(q, k, scratch, *(out or ()))
+    if q.dtype != torch.bfloat16 or k.dtype != torch.bfloat16:
+        raise ValueError("bf16 tensors required")
+    st = q.stride()
+    if st != k.stride() or st[2] != 1:
+        raise ValueError("q and k must share strides with a contiguous last dimension")
+    bt, bh, bw = tile
+    if bt < 1 or bh < 1 or bw < 1:
+        raise ValueError("tile extents must be positive")
+    nb = -(-T // bt) * -(-H // bh) * -(-W // bw)
+    each = [int(keep)] * nh if not hasattr(keep, "__len__") else [int(x) for x in keep]
+    if len(each) != nh or min(each) < 1 or max(each) > nb:
+        raise ValueError("keep: between 1 and the number of blocks, one for all heads or one each")
+    prob = _problem(nh, tile, 1.0, st[0], st[1], d)
+    need = int(lib().psa_select_scratch_bytes(prob, T, H, W))
+    if need < 0:
+        _check(need, "psa_select_blocks")
+    new = []
+    if out is None:
+        out = (torch.empty(nh * nb + 1, dtype=torch.int32, device=q.device), torch.empty(sum(each) * nb, dtype=torch.int32, device=q.device))
+        new.extend(out)
+    row_ptr, col_idx = out
+    if any(x.dtype != torch.int32 or not x.is_contiguous() for x in out) or row_ptr.numel() != nh * nb + 1 or col_idx.numel() < sum(each) * nb:
+        raise ValueError("row_ptr (heads * blocks + 1 entries) and col_idx must be contiguous int32 tensors")
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        new.append(scratch)
+    elif scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
+        raise ValueError("scratch too small")
+    _used_on(stream, *new)
+    _check(lib().psa_select_blocks(q.data_ptr(), k.data_ptr(), prob, T, H, W, struct.pack("%di" % nh, *each), 1 if keep_self else 0, row_ptr.data_ptr(),
+                                   col_idx.data_ptr(), col_idx.numel(), scratch.data_ptr(), _stream_ptr(stream)), "psa_select_blocks")
+    return row_ptr, col_idx
+
+
+def psa_attn_fwd_lists_scratch_bytes(n_heads: int, grid: Sequence[int], tile: Sequence[int], n_text: int = 0) -> int:
+    """Bytes of device scratch that psa_attn_fwd_lists needs."""
+    T, H, W = map(int, grid)
+    n = int(lib().psa_attn_fwd_lists_scratch_bytes(_problem(n_heads, tile, 1.0, 0, 128), int(n_text), T, H, W))
+    if n < 0:
+        _check(n, "psa_attn_fwd_lists_scratch_bytes")
+    return n
+
+
+def psa_attn_fwd_lists(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_ptr: torch.Tensor, col_idx: torch.Tensor, grid: Sequence[int],
+                       tile: Sequence[int], scale: float, n_text: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       scratch: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Attention over lists of key blocks (see psa.h): q, k, v are bf16 device tensors [heads, T*H*W + n_text, 128] sharing strides, the
+    video tokens first; query block i of head h attends the blocks ``col_idx[row_ptr[h*NB + i]:row_ptr[h*NB + i + 1]]`` (int32,
+    ascending), as psa_mask_build and psa_select_blocks write them, and all of the text.  ``scratch`` (uint8,
+    psa_attn_fwd_lists_scratch_bytes long) is allocated when not given.  Returns (out like q, lse fp32 [heads, tokens])."""
+    nh, Lt, d = q.shape
+    T, H, W = map(int, grid)
+    n_text = int(n_text)
+    if Lt != T * H * W + n_text or k.shape != q.shape or v.shape != q.shape:
+        raise ValueError("shape mismatch")
+    _on_current_device(q, k, v, row_ptr, col_idx, out, lse, scratch)
+    bt, bh, bw = tile
+    if bt < 1 or bh < 1 or bw < 1:
+        raise ValueError("tile extents must be positive")
+    nb = -(-T // bt) * -(-H // bh) * -(-W // bw)
+    i32 = torch.int32
+    if row_ptr.dtype != i32 or col_idx.dtype != i32 or not row_ptr.is_contiguous() or not col_idx.is_contiguous() or row_ptr.numel() != nh * nb + 1:
+        raise ValueError("row_ptr (heads * blocks + 1 entries) and col_idx must be contiguous int32 tensors")
+    mine = (out, lse)
+    if (out is not None and (out.shape != q.shape or out.dtype != q.dtype)) or (lse is not None and (tuple(lse.shape) != (nh, Lt) or lse.dtype != torch.float32)):
+        raise ValueError("out must be like q, lse fp32 [heads, tokens]")
+    out, lse, st = _device_call(q, k, v, out, lse, (nh, Lt))
+    prob = _problem(nh, tile, scale, st[0], st[1], d)
+    need = int(lib().psa_attn_fwd_lists_scratch_bytes(prob, n_text, T, H, W))
+    if need < 0:
+        _check(need, "psa_attn_fwd_lists")
+    given = scratch
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
+        raise ValueError("scratch too small")
+    if stream is not None:
+        _used_on(stream, *(t for t, m in zip((out, lse, scratch), (*mine, given)) if m is None))
+    _check(lib().psa_attn_fwd_lists(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), row_ptr.data_ptr(), col_idx.data_ptr(),
+                                    col_idx.numel(), prob, n_text, T, H, W, scratch.data_ptr(), _stream_ptr(stream)), "psa_attn_fwd_lists")
+    return out, lse
 
 
 LAUNCH_MODES = ("ticket", "direct", "shared", "shared_direct", "ticket_edge", "ticket_short")

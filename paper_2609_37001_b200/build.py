@@ -15,7 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpsa.so")
 LIB_CHECKED = os.path.join(HERE, "libpsa_checked.so")
-SOURCES = ["psa_host.cu", "psa_mask_build.cu", "psa_attn_sm100.cu", "psa_search.cu", "psa_norm_rope.cu"]
+SOURCES = ["psa_host.cu", "psa_mask_build.cu", "psa_attn_sm100.cu", "psa_search.cu", "psa_norm_rope.cu", "psa_select.cu"]
 HEADERS = [os.path.join(CSRC, "psa_common.cuh"), os.path.join(CSRC, "psa_norm_rope.cuh"), os.path.join(ROOT, "include", "psa.h")]
 
 

@@ -407,6 +407,16 @@ __device__ __forceinline__ uint32_t last_row_word(const Geom& g, int b) {
   return !(g.edge_axes & 2) || d >= 32 ? 0u : (d <= 0 ? 0xffffffffu : 0xffffffffu << d);
 }
 
+// The list of row r (head * NB + query block): its first entry and its length.  Lists come from the caller's device memory: a row
+// that does not lie within the entries, or is longer than there are blocks, counts as empty (false).
+__device__ __forceinline__ bool list_of(const KeyLists& l, const Geom& g, long long r, int* start, int* n) {
+  const int from = l.row_ptr[r], to = l.row_ptr[r + 1];
+  const bool good = from >= 0 && from <= to && to <= l.n_entries && to - from <= g.NB;
+  *start = from;
+  *n = good ? to - from : 0;
+  return good;
+}
+
 // ----------------------------------------------------------------------------- planning
 // Work order: heads by descending number of attended pairs (`place`, from the host; heads stay together so that
 // concurrently running CTAs share K/V in L2), within a head query blocks by descending number of attended key blocks.
@@ -419,6 +429,50 @@ __host__ __device__ __forceinline__ int plan_key_words(const Geom& g) {
   const int sets = axis_words(g.Tp) + axis_words(g.Sp);
   return g.NB > sets ? g.NB : sets;
 }
+// A head's items by its blocks' keys: writes those of head h to its place in the work order (all threads of a planning block).
+__device__ __forceinline__ void order_items(const Geom& g, int h, int place, const uint32_t* key, WorkItem* __restrict__ items) {
+  const int ipb = g.items_per_block;
+  // Text-query items of all heads first: they attend every key block, so they are the heaviest (behind the lighter
+  // items of earlier heads the last one alone kept the launch running: 825 instead of 783 us for 7 heads of 150 blocks).
+  // Two text slabs per item; a single one runs in split-KV mode.  Flag in bit 25.
+  WorkItem* head_items = items + (size_t)place * g.n_titems;
+  for (int it = threadIdx.x; it < g.n_titems; it += kPlanThreads) {
+    const int sub0 = 2 * it;
+    const int nq = (g.n_ts - sub0) >= 2 ? 2 : 1;
+    head_items[it] = make_int4(h, 0, g.NB, sub0 | (nq << 16) | ((nq == 1 ? 1 : 0) << 24) | (1 << 25));
+  }
+  WorkItem* out = items + (size_t)gridDim.x * g.n_titems + (size_t)place * (g.items_per_head - g.n_titems);
+  for (int qb = threadIdx.x; qb < g.NB; qb += kPlanThreads) {
+    const uint32_t mine = key[qb];
+    int pos = 0, j = 0;
+    for (; j + 4 <= g.NB; j += 4) {
+      const uint4 k4 = *reinterpret_cast<const uint4*>(key + j);
+      pos += (int)(k4.x > mine) + (int)(k4.y > mine) + (int)(k4.z > mine) + (int)(k4.w > mine);
+    }
+    for (; j < g.NB; ++j) pos += (int)(key[j] > mine);
+    const int c = (int)(mine / (uint32_t)g.NB);
+    const int n_sub = g.slabs_of[block_class(g, qb / g.Sp, qb % g.Sp)];
+    // two-slab items first (heavier), then the odd single-slab items, each in rank order
+    for (int it = 0; it < ipb; ++it) {
+      const int sub0 = 2 * it;
+      if (sub0 >= n_sub) break;
+      if (it == 1 && g.items_per_head - g.n_titems != 2 * g.NB) {   // some blocks have no second item: the rank among those that have one
+        pos = j = 0;
+        for (int tj = 0; tj < g.Tp; ++tj)
+          for (int sj = 0, wj = 0; sj < g.Sp; ++sj, ++j) {
+            const int cj = g.edge_axes & ((tj == g.Tp - 1 ? 1 : 0) | (sj >= g.s_edge ? 2 : 0) | (wj == g.Wp - 1 ? 4 : 0));
+            pos += (int)(g.slabs_of[cj] > 2 && key[j] > mine);
+            wj = wj == g.Wp - 1 ? 0 : wj + 1;
+          }
+      }
+      const int nq = (n_sub - sub0) >= 2 ? 2 : 1;
+      // A single-slab item runs in split-KV mode: both softmax warpgroups work on that one
+      // query slab, one on the even and one on the odd key slabs (flag in bit 24).
+      out[(size_t)it * g.NB + pos] = make_int4(h, qb, c, sub0 | (nq << 16) | ((nq == 1 ? 1 : 0) << 24));
+    }
+  }
+}
+
 __global__ void __launch_bounds__(kPlanThreads)
 plan_kernel(const __grid_constant__ PlanParams hp, const Geom g, int* __restrict__ ws_header,
             psa_head_params* __restrict__ hp_dev, WorkItem* __restrict__ items) {
@@ -468,46 +522,25 @@ plan_kernel(const __grid_constant__ PlanParams hp, const Geom g, int* __restrict
   for (int qb = threadIdx.x; qb < g.NB; qb += kPlanThreads)
     key[qb] = cntT[qb / g.Sp] * cntS[qb % g.Sp] * (uint32_t)g.NB + (uint32_t)(g.NB - 1 - qb);
   __syncthreads();
-  const int ipb = g.items_per_block;
-  // Text-query items of all heads first: they attend every key block, so they are the heaviest (behind the lighter
-  // items of earlier heads the last one alone kept the launch running: 825 instead of 783 us for 7 heads of 150 blocks).
-  // Two text slabs per item; a single one runs in split-KV mode.  Flag in bit 25.
-  WorkItem* head_items = items + (size_t)hp.place[h] * g.n_titems;
-  for (int it = threadIdx.x; it < g.n_titems; it += kPlanThreads) {
-    const int sub0 = 2 * it;
-    const int nq = (g.n_ts - sub0) >= 2 ? 2 : 1;
-    head_items[it] = make_int4(h, 0, g.NB, sub0 | (nq << 16) | ((nq == 1 ? 1 : 0) << 24) | (1 << 25));
-  }
-  WorkItem* out = items + (size_t)gridDim.x * g.n_titems + (size_t)hp.place[h] * (g.items_per_head - g.n_titems);
+  order_items(g, h, hp.place[h], key, items);
+}
+
+// The same for lists of key blocks (psa_attn_fwd_lists): the counts are the lists' lengths, and heads keep their order, as
+// their weights are not known to the host.
+__global__ void __launch_bounds__(kPlanThreads)
+plan_lists_kernel(const Geom g, const KeyLists lists, int* __restrict__ counter, int* __restrict__ ws_header, int call_id, WorkItem* __restrict__ items) {
+  extern __shared__ __align__(16) uint32_t sm[];
+  pdl_trigger();
+  const int h = blockIdx.x;
+  pdl_wait();
+  if (h == 0 && threadIdx.x == 0) *counter = 0;
   for (int qb = threadIdx.x; qb < g.NB; qb += kPlanThreads) {
-    const uint32_t mine = key[qb];
-    int pos = 0, j = 0;
-    for (; j + 4 <= g.NB; j += 4) {
-      const uint4 k4 = *reinterpret_cast<const uint4*>(key + j);
-      pos += (int)(k4.x > mine) + (int)(k4.y > mine) + (int)(k4.z > mine) + (int)(k4.w > mine);
-    }
-    for (; j < g.NB; ++j) pos += (int)(key[j] > mine);
-    const int c = (int)(mine / (uint32_t)g.NB);
-    const int n_sub = g.slabs_of[block_class(g, qb / g.Sp, qb % g.Sp)];
-    // two-slab items first (heavier), then the odd single-slab items, each in rank order
-    for (int it = 0; it < ipb; ++it) {
-      const int sub0 = 2 * it;
-      if (sub0 >= n_sub) break;
-      if (it == 1 && g.items_per_head - g.n_titems != 2 * g.NB) {   // some blocks have no second item: the rank among those that have one
-        pos = j = 0;
-        for (int tj = 0; tj < g.Tp; ++tj)
-          for (int sj = 0, wj = 0; sj < g.Sp; ++sj, ++j) {
-            const int cj = g.edge_axes & ((tj == g.Tp - 1 ? 1 : 0) | (sj >= g.s_edge ? 2 : 0) | (wj == g.Wp - 1 ? 4 : 0));
-            pos += (int)(g.slabs_of[cj] > 2 && key[j] > mine);
-            wj = wj == g.Wp - 1 ? 0 : wj + 1;
-          }
-      }
-      const int nq = (n_sub - sub0) >= 2 ? 2 : 1;
-      // A single-slab item runs in split-KV mode: both softmax warpgroups work on that one
-      // query slab, one on the even and one on the odd key slabs (flag in bit 24).
-      out[(size_t)it * g.NB + pos] = make_int4(h, qb, c, sub0 | (nq << 16) | ((nq == 1 ? 1 : 0) << 24));
-    }
+    int start, n;
+    if (!list_of(lists, g, (long long)h * g.NB + qb, &start, &n)) report_status(ws_header, call_id, PSA_ERR_INVALID_ARG, kBadListRow);
+    sm[qb] = (uint32_t)n * (uint32_t)g.NB + (uint32_t)(g.NB - 1 - qb);
   }
+  __syncthreads();
+  order_items(g, h, h, sm, items);
 }
 
 // ----------------------------------------------------------------------------- attention
@@ -852,12 +885,19 @@ __device__ __forceinline__ void merge_cluster(const Params& prm, const uint8_t* 
 //                 12 heads of 1x8x16 blocks attending 19.5 of them, 8x32x48 grid: 221 -> 198 us
 // (A slab of a cut grid goes through a list of boxes, which costs the load warp some 700 clocks: more than it has in split-KV mode.
 // 2 heads of 5x16x63 with 1x30x8 blocks, one slab each, took 28.6 us as a cut grid and take 23.6 as a padded one.)
-template <int kGrid> struct ArgsOf { typedef TensorMaps maps; typedef AttnParams params; };
-template <> struct ArgsOf<kCut> { typedef TensorMapsCut maps; typedef AttnParamsCut params; };
-template <int kMode, int kGrid>
+// kByList: the key blocks of an item are those of its row in the caller's lists (psa_attn_fwd_lists) instead of the stripes'.  The
+// load warp reads 32 entries at a time, one a lane, the next ones while these are loaded, and each lane works out its
+// block's origin.  Every block counts as one of the pattern: slabs without tokens are zeros with validity bits of 0.
+template <int kGrid, bool kByList> struct ArgsOf { typedef TensorMaps maps; typedef AttnParams params; };
+template <> struct ArgsOf<kCut, false> { typedef TensorMapsCut maps; typedef AttnParamsCut params; };
+template <int kGrid> struct ArgsOf<kGrid, true> { typedef TensorMaps maps; typedef AttnParamsLists params; };
+struct NoHeads {};
+template <bool kByList> struct HeadsOf { typedef HeadParamsArray type; };
+template <> struct HeadsOf<true> { typedef NoHeads type; };
+template <int kMode, int kGrid, bool kByList = false>
 __global__ void __launch_bounds__(kThreads, 1)
-attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid>::maps tms, const __grid_constant__ HeadParamsArray heads,
-                const __grid_constant__ typename ArgsOf<kGrid>::params prm) {
+attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid, kByList>::maps tms, const __grid_constant__ typename HeadsOf<kByList>::type heads,
+                const __grid_constant__ typename ArgsOf<kGrid, kByList>::params prm) {
   // 128-byte swizzled slabs need a 1024-byte aligned base; the declaration asks for it and the
   // kernel checks it (a misaligned base is reported through the status word, no work is done).
   constexpr bool kCluster = kMode == kShared || kMode == kSharedDirect, kShort = kMode == kTicketShort;
@@ -916,7 +956,8 @@ attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid>::maps tms, const 
   if constexpr (!kPlanned) {
     if (warp == kWarpLoad) {
       first_item = direct_item<kEdge>(g, (int)(blockIdx.x / cluster_size()), lane);
-      attended = key_block_sets<kEdge>(g, ((first_item.w >> 25) & 1) != 0, first_item.y, heads.p[first_item.x], lane, maskT, maskS);
+      if constexpr (!kByList)
+        attended = key_block_sets<kEdge>(g, ((first_item.w >> 25) & 1) != 0, first_item.y, heads.p[first_item.x], lane, maskT, maskS);
     }
   }
   // A persistent CTA has one idle thread wait for the kernel before, on behalf of every role behind the barrier.  (Waits in
@@ -978,7 +1019,7 @@ attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid>::maps tms, const 
     if constexpr (kBoxes) {
       n_classes = prm.n_classes;
       late = late || !prm.planned;
-    } else if constexpr (kEdge) {
+    } else if constexpr (kEdge && !kByList) {
       n_classes = g.edge_axes != 0 ? 2 : 1;
       late = late || g.edge_axes != 0;
     }
@@ -1045,20 +1086,39 @@ attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid>::maps tms, const 
       };
       if constexpr (kDraws) {
         if (lane == 0) {
-          const int ticket = atomicAdd(prm.ws_header + kWsCounter, 1);
+          int* counter;
+          if constexpr (kByList) counter = prm.counter;
+          else counter = prm.ws_header + kWsCounter;
+          const int ticket = atomicAdd(counter, 1);
           if (ticket < prm.n_items) wi = prm.items[ticket];
           if (!late) publish();
         }
         wi.x = __shfl_sync(0xffffffffu, wi.x, 0);
         wi.y = __shfl_sync(0xffffffffu, wi.y, 0);
-        wi.w = __shfl_sync(0xffffffffu, wi.w, 0);
+        wi.w = __shfl_sync(0xffffffffu, wi.w, 0);   // (z is counted again)
       } else if (n == 0) {
         wi = kPlanned ? prm.items[blockIdx.x / cluster_size()] : first_item;
       }
+      int list_start = 0;
+      if constexpr (kByList) {
+        if (wi.x >= 0) {
+          wi.z = g.NB;   // (text queries)
+          if (((wi.w >> 25) & 1) == 0 && !list_of(prm.lists, g, (long long)wi.x * g.NB + wi.y, &list_start, &wi.z) && lane == 0 && !kPlanned)
+            report_status(prm.ws_header, prm.call_id, PSA_ERR_INVALID_ARG, kBadListRow);
+          if constexpr (kCluster) {   // (shares of at most 2^16 blocks by 8)
+            const int r = (int)cluster_rank(), shift = 31 - __clz((int)cluster_size()), all = wi.z;
+            skip = all * r >> shift;
+            wi.z = (all * (r + 1) >> shift) - skip;
+            if (r + 1 < (int)cluster_size()) wi.w |= 1 << 26;
+          }
+        }
+        if (late && lane == 0) publish();
+      } else {
       if (kPlanned && wi.x >= 0) attended = key_block_sets<kEdge>(g, ((wi.w >> 25) & 1) != 0, wi.y, prm.hp_dev[wi.x], lane, maskT, maskS);
       if (late) {
         if (wi.x >= 0) take_share();
         if (lane == 0) publish();
+      }
       }
       if (wi.x < 0) break;
       const int head = kEdge ? wi.x & 0xff : wi.x, qb = wi.y, sub0 = wi.w & 0xffff, nq = (wi.w >> 16) & 0xff;
@@ -1209,6 +1269,56 @@ attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid>::maps tms, const 
         issued(n, 0, 0, 0, ntok);
         list = list == kLists - 1 ? 0 : list + 1;
       };
+      if constexpr (kByList) {
+        const int* entries = prm.lists.col_idx + list_start + skip;
+        const int n = wi.z, n_slabs = kEdge ? g.main_slabs : g.n_sub;
+        int before = !textq && skip > 0 && n > 0 ? entries[-1] : -1;   // the entry before the 32
+        auto entry = [&](int i) -> int { return i >= n ? 0 : (textq ? skip + i : entries[i]); };
+        int ahead = entry(lane);
+#pragma unroll 1
+        for (int base = 0; ok && base < n; base += 32) {
+          const int id = ahead;
+          ahead = entry(base + 32 + lane);
+          // entries come from the caller's memory: one that is no block, or does not come behind its neighbour, is left out
+          int left_of = __shfl_up_sync(0xffffffffu, id, 1);
+          if (lane == 0) left_of = before;
+          before = __shfl_sync(0xffffffffu, id, 31);
+          const bool good = id >= 0 && id < g.NB && id > left_of;
+          const uint32_t taken = __ballot_sync(0xffffffffu, good);
+          if (base + lane < n && !good) report_status(prm.ws_header, prm.call_id, PSA_ERR_INVALID_ARG, kBadListEntry);
+          const int tk = good ? id / g.Sp : 0, sk = good ? id - tk * g.Sp : 0, hb = (int)(((unsigned long long)(uint32_t)sk * magic_w) >> 22);
+          const int mine_t = good ? tk * g.bt : g.T, mine_h = hb * g.bh, mine_w = (sk - hb * g.Wp) * g.bw;   // (from frame T on: zeros)
+          const int here = n - base < 32 ? n - base : 32;
+#pragma unroll 1
+          for (int j = 0; ok && j < here; ++j) {
+            int t0 = __shfl_sync(0xffffffffu, mine_t, j), h0 = __shfl_sync(0xffffffffu, mine_h, j), w0 = __shfl_sync(0xffffffffu, mine_w, j);
+            const bool in = (taken >> j) & 1u;
+#pragma unroll 1
+            for (int sub = 0; ok && sub < n_slabs; ++sub) {
+              const int last = (sub == g.n_sub - 1) ? 1 : 0, ntok = last ? g.n_last : kSlabTokens;
+              uint32_t vw[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+              bool cut = !in;
+              if constexpr (kGrid == kPadded) {
+                const int et = last && g.sub_axis == 0 ? g.c_last : g.ct, eh = last && g.sub_axis == 1 ? g.c_last : g.ch,
+                          ew = last && g.sub_axis == 2 ? g.c_last : g.cw;
+                cut = cut || et > g.T - t0 || eh > g.H - h0 || ew > g.W - w0;
+              }
+              if (cut) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int x = lane + 32 * i;
+                  const bool inside = in && (x >> g.pos_ts) < g.T - t0 && ((x >> g.pos_ws) & (g.ch - 1)) < g.H - h0 && (x & (g.cw - 1)) < g.W - w0;
+                  vw[i] = __ballot_sync(0xffffffffu, inside || x >= ntok);
+                }
+              }
+              issue_slab(t0, h0, w0, last, ntok, vw[0], vw[1], vw[2], vw[3]);
+              if (g.sub_axis == 0) t0 += g.ct;
+              else if (g.sub_axis == 1) h0 += g.ch;
+              else w0 += g.cw;
+            }
+          }
+        }
+      } else {
       // classes in turn
       int before = 0;
 #pragma unroll 1
@@ -1304,6 +1414,7 @@ attn_fwd_kernel(const __grid_constant__ typename ArgsOf<kGrid>::maps tms, const 
             }
           }
         }
+      }
       }
       }
       // text key slabs: attended by every query; tokens beyond n_text are zero-filled and masked
@@ -1988,7 +2099,10 @@ struct LaunchConfig {
 cudaError_t attn_init(int clusters[3]) {
 #define PSA_ALL_GRIDS(mode) (const void*)attn_fwd_kernel<mode, kWhole>, (const void*)attn_fwd_kernel<mode, kPadded>, (const void*)attn_fwd_kernel<mode, kCut>
   const void* kernels[] = {PSA_ALL_GRIDS(kTicket), PSA_ALL_GRIDS(kDirect), PSA_ALL_GRIDS(kShared), PSA_ALL_GRIDS(kSharedDirect),
-                           (const void*)attn_fwd_kernel<kTicketShort, kWhole>, (const void*)attn_fwd_kernel<kTicketShort, kPadded>};
+                           (const void*)attn_fwd_kernel<kTicketShort, kWhole>, (const void*)attn_fwd_kernel<kTicketShort, kPadded>,
+#define PSA_LIST_GRIDS(mode) (const void*)attn_fwd_kernel<mode, kWhole, true>, (const void*)attn_fwd_kernel<mode, kPadded, true>
+                           PSA_LIST_GRIDS(kTicket), PSA_LIST_GRIDS(kDirect), PSA_LIST_GRIDS(kSharedDirect)};
+#undef PSA_LIST_GRIDS
 #undef PSA_ALL_GRIDS
   cudaError_t e = cudaSuccess;
   for (const void* k : kernels)
@@ -2026,6 +2140,28 @@ cudaError_t launch_mode(const LaunchConfig& lc, Grid grid, const TensorMapsCut& 
   const AttnParams& p = prm;
   if (grid == kPadded) return cudaLaunchKernelEx(&lc.cfg, attn_fwd_kernel<kMode, kPadded>, plain, heads, p);
   return cudaLaunchKernelEx(&lc.cfg, attn_fwd_kernel<kMode, kWhole>, plain, heads, p);
+}
+
+// Attention over lists: planned items drawn by persistent CTAs, or (direct) one item a CTA or cluster, in the order of heads and blocks.
+cudaError_t launch_plan_lists(const Geom& g, const KeyLists& lists, int n_heads_here, int* counter, int* ws_header, int call_id, WorkItem* items,
+                              cudaStream_t stream) {
+  LaunchConfig lc(n_heads_here, kPlanThreads, sizeof(uint32_t) * (size_t)g.NB, stream, 1);
+  if (lc.cfg.dynamicSmemBytes > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(plan_lists_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lc.cfg.dynamicSmemBytes);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaLaunchKernelEx(&lc.cfg, plan_lists_kernel, g, lists, counter, ws_header, call_id, items);
+}
+cudaError_t launch_attn_lists(const TensorMaps& tm, const AttnParamsLists& prm, int n_sms, int cluster, Grid grid, bool direct, cudaStream_t stream,
+                              Mode* mode) {
+  const int ctas = cluster > 1 || direct ? prm.n_items * cluster : (prm.n_items < n_sms ? prm.n_items : n_sms);
+  LaunchConfig lc(ctas, kThreads, kSmemAlloc, stream, cluster);
+  *mode = cluster > 1 ? kSharedDirect : (direct ? kDirect : kTicket);
+  const NoHeads none;
+  auto launch = [&](auto* whole, auto* padded) { return cudaLaunchKernelEx(&lc.cfg, grid == kWhole ? whole : padded, tm, none, prm); };
+  if (*mode == kSharedDirect) return launch(attn_fwd_kernel<kSharedDirect, kWhole, true>, attn_fwd_kernel<kSharedDirect, kPadded, true>);
+  if (*mode == kDirect) return launch(attn_fwd_kernel<kDirect, kWhole, true>, attn_fwd_kernel<kDirect, kPadded, true>);
+  return launch(attn_fwd_kernel<kTicket, kWhole, true>, attn_fwd_kernel<kTicket, kPadded, true>);
 }
 
 // heads: read by launches without planning only.  cluster: CTAs per work item, 1: whole items.  direct: all items run

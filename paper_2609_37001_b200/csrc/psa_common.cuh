@@ -125,6 +125,25 @@ struct AttnParamsCut : AttnParams {
   uint8_t order[8];
 };
 
+// Blocks that psa_select_blocks keeps for each query block of a head, and the head's first entry of col_idx.
+struct SelectHeads {
+  int keep[kMaxHeads], base[kMaxHeads];
+};
+
+// Lists of key blocks in the caller's device memory: row r = head * NB + query block is col_idx[row_ptr[r] .. row_ptr[r + 1] - 1].
+struct KeyLists {
+  const int* row_ptr;
+  const int* col_idx;
+  int n_entries;
+};
+constexpr int kBadListRow = 0x600, kBadListEntry = 0x601;   // details of PSA_ERR_INVALID_ARG that the kernels report
+
+// The arguments of a launch over lists; those of the launch's first head on.
+struct AttnParamsLists : AttnParams {
+  KeyLists lists;
+  int* counter;                // scheduler ticket
+};
+
 // Layout of the per-device workspace (all int32 words).
 constexpr int kWsStatus = 0;     // first device-side error of call kWsCallId
 constexpr int kWsDetail = 1;     // diagnostic of that error

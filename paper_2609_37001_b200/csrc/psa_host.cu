@@ -24,6 +24,13 @@ cudaError_t launch_plan(const PlanParams& hp, const Geom& g, int n_heads_here, i
                         WorkItem* items, cudaStream_t stream);
 cudaError_t launch_attn(const TensorMapsCut& tm, const HeadParamsArray& heads, const AttnParamsCut& prm, int n_sms, int cluster,
                         Grid grid, bool direct, bool short_items, bool empty_slabs, cudaStream_t stream, Mode* mode);
+cudaError_t launch_plan_lists(const Geom& g, const KeyLists& lists, int n_heads_here, int* counter, int* ws_header, int call_id, WorkItem* items,
+                              cudaStream_t stream);
+cudaError_t launch_attn_lists(const TensorMaps& tm, const AttnParamsLists& prm, int n_sms, int cluster, Grid grid, bool direct, cudaStream_t stream,
+                              Mode* mode);
+bool select_fits(int nb);
+cudaError_t launch_select(const void* q, const void* k, const Geom& g, long long stride_head, long long stride_token, const SelectHeads& heads, int n_heads,
+                          bool keep_self, double* sums, int* row_ptr, int* col_idx, cudaStream_t st, int* launches);
 size_t search_partial_bytes(int n_cand);
 cudaError_t launch_search_losses(const void* outs, const void* ref, long long elems_per_cand, int n_cand, double* partial,
                                  float* losses, cudaStream_t stream, int* launches);
@@ -44,6 +51,7 @@ struct Workspace {
   int n_sms = 0;
   int cc_major = 0;
   int last_call = 0;             // id of the last API call whose kernels report to the status words
+  bool last_lists = false;       // which reported to those of calls over lists
   bool attn_ready = false;
   int clusters[3] = {0, 0, 0};   // clusters of 2, 4 and 8 attention CTAs that run at a time
 };
@@ -704,6 +712,24 @@ bool short_items(const HostGeom& g, const long long* weights, int n_heads) {
   return g.n_sub == 1 && (double)total * slabs_per_block(g) < (64.0 - g.n_ts) * n_heads * g.NB;
 }
 
+// g_last_attn of a launch (but for its mode).  lists: every key block counts as one of the pattern.
+void record_launch(const HostGeom& hg, int n_items, int cluster, bool lists) {
+  g_last_attn.items = n_items;
+  g_last_attn.cluster = cluster;
+  g_last_attn.grid = hg.grid;
+  g_last_attn.slabs = hg.main_slabs;
+  g_last_attn.last_keys = hg.main_last;
+  g_last_attn.edge_axes = hg.edge_axes;
+  for (int c = 0; c < 8; ++c) {
+    const int slabs = class_blocks(hg, c) ? hg.slabs_of[c] : 0;
+    const bool follows = hg.grid == kCut ? hg.cls[c].in_pattern != 0 : slabs == hg.main_slabs;
+    g_last_attn.query_slabs[c] = (uint8_t)slabs;
+    g_last_attn.together[c] = hg.grid == kCut && slabs ? hg.cls[c].together : 1;
+    g_last_attn.keys[c] = (uint16_t)(slabs == 0 ? 0 : lists ? (hg.main_slabs - 1) * kSlabTokens + hg.main_last
+                                                            : (slabs - 1) * kSlabTokens + (follows ? hg.main_last : kSlabTokens));
+  }
+}
+
 // Planning (unless the launch is direct) and attention.
 cudaError_t launch_call(const TensorMapsCut& tm, const AttnParams& prm, const HostGeom& hg, const psa_head_params* params, const long long* weights,
                         const Workspace& ws, int cluster, bool record, cudaStream_t st) {
@@ -733,21 +759,25 @@ cudaError_t launch_call(const TensorMapsCut& tm, const AttnParams& prm, const Ho
                                     &g_last_attn.mode);
   if (e == cudaSuccess) {
     ++g_launches;
-    g_last_attn.items = prm.n_items;
-    g_last_attn.cluster = cluster;
-    g_last_attn.grid = hg.grid;
-    g_last_attn.slabs = hg.main_slabs;
-    g_last_attn.last_keys = hg.main_last;
-    g_last_attn.edge_axes = hg.edge_axes;
-    for (int c = 0; c < 8; ++c) {
-      const int slabs = class_blocks(hg, c) ? hg.slabs_of[c] : 0;
-      const bool follows = hg.grid == kCut ? hg.cls[c].in_pattern != 0 : slabs == hg.main_slabs;
-      g_last_attn.query_slabs[c] = (uint8_t)slabs;
-      g_last_attn.together[c] = hg.grid == kCut && slabs ? hg.cls[c].together : 1;
-      g_last_attn.keys[c] = (uint16_t)(slabs == 0 ? 0 : (slabs - 1) * kSlabTokens + (follows ? hg.main_last : kSlabTokens));
-    }
+    record_launch(hg, prm.n_items, cluster, false);
   }
   return e;
+}
+
+// Planning (unless the launch is direct) and attention over lists.
+cudaError_t launch_lists(const TensorMaps& tm, const AttnParamsLists& prm, const HostGeom& hg, const Workspace& ws, int cluster, bool direct, cudaStream_t st) {
+  if (!direct) {
+    const cudaError_t e = launch_plan_lists(prm.g, prm.lists, prm.g.n_heads, prm.counter, prm.ws_header, prm.call_id, const_cast<WorkItem*>(prm.items), st);
+    if (e != cudaSuccess) return e;
+    ++g_launches;
+  }
+  if (g_ev_start && g_ev_stop) cudaEventRecord(g_ev_start, st);
+  const cudaError_t e = launch_attn_lists(tm, prm, ws.n_sms, cluster, hg.grid, direct, st, &g_last_attn.mode);
+  if (e != cudaSuccess) return e;
+  ++g_launches;
+  record_launch(hg, prm.n_items, cluster, true);
+  if (g_ev_start && g_ev_stop) cudaEventRecord(g_ev_stop, st);
+  return cudaSuccess;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -790,6 +820,19 @@ static __device__ __align__(256) unsigned char g_noalloc_scratch[kNoAllocBytes];
 // Device address of the array, looked up once per device with that device current.  In host
 // code the array's name is only a handle for the runtime, never an address a kernel may use.
 void* g_noalloc_ptr[kMaxDevices] = {};
+
+// Status words of calls over lists, which have no workspace of the library's: they stay where they are from load to exit.
+static __device__ __align__(16) int g_lists_status[kWsHeaderWords];
+int* g_lists_status_ptr[kMaxDevices] = {};
+int lists_status(int dev, int** ptr) {
+  if (!g_lists_status_ptr[dev]) {
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_lists_status) != cudaSuccess || p == nullptr) return PSA_ERR_CUDA;
+    g_lists_status_ptr[dev] = static_cast<int*>(p);
+  }
+  *ptr = g_lists_status_ptr[dev];
+  return PSA_OK;
+}
 
 int noalloc_scratch(int dev, void** ptr) {
   if (!g_noalloc_ptr[dev]) {
@@ -949,7 +992,10 @@ static int run_attn(const void* q, const void* k, const void* v, void* out, floa
     const int chosen = choose_edges(*ws, &g, weights.data(), n_heads);
     cluster = cluster < 0 ? 1 : chosen;
   }
-  if (new_call) ws->last_call = next_call_id(st);
+  if (new_call) {
+    ws->last_call = next_call_id(st);
+    ws->last_lists = false;
+  }
   for (int head0 = 0; head0 < n_heads; head0 += kMaxHeads) {
     const int n_here = n_heads - head0 < kMaxHeads ? n_heads - head0 : kMaxHeads;
     const long long in_off = lay.shared_qkv ? 0 : (long long)head0 * lay.in_head;
@@ -993,6 +1039,117 @@ static int attn_fwd_checked(const void* q, const void* k, const void* v, void* o
 int psa_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse, const psa_head_params* head_params,
                  const psa_problem* prob, int T, int H, int W, void* stream) {
   return attn_fwd_checked(q, k, v, out, lse, head_params, prob, T, H, W, stream, true);
+}
+
+static size_t select_bytes(const HostGeom& g) { return 2 * sizeof(double) * kHeadDim * (size_t)(g.n_heads < kMaxHeads ? g.n_heads : kMaxHeads) * g.NB; }
+
+int64_t psa_select_scratch_bytes(const psa_problem* prob, int T, int H, int W) {
+  HostGeom g;
+  const int rc = make_geom(prob, T, H, W, false, &g);
+  if (rc != PSA_OK) return rc;
+  return select_fits(g.NB) ? (int64_t)select_bytes(g) : PSA_ERR_UNSUPPORTED;
+}
+
+int psa_select_blocks(const void* q, const void* k, const psa_problem* prob, int T, int H, int W, const int32_t* keep, int keep_self, int32_t* row_ptr,
+                      int32_t* col_idx, int64_t col_capacity, void* scratch, void* stream) {
+  HostGeom g;
+  int rc = make_geom(prob, T, H, W, false, &g);
+  if (rc != PSA_OK) return rc;
+  if (!q || !k || !keep || !row_ptr || !col_idx || !scratch) return PSA_ERR_INVALID_ARG;
+  if (prob->head_dim != kHeadDim || !select_fits(g.NB)) return PSA_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(scratch) || (reinterpret_cast<uintptr_t>(row_ptr) & 3u) || (reinterpret_cast<uintptr_t>(col_idx) & 3u))
+    return PSA_ERR_INVALID_ARG;
+  if (prob->stride_token < kHeadDim || (prob->stride_token % 8) != 0) return PSA_ERR_INVALID_ARG;
+  if (prob->n_heads > 1 && (prob->stride_head < kHeadDim || (prob->stride_head % 8) != 0)) return PSA_ERR_INVALID_ARG;
+  long long total = 0;
+  for (int h = 0; h < prob->n_heads; ++h) {
+    if (keep[h] < 1 || keep[h] > g.NB) return PSA_ERR_INVALID_ARG;
+    total += (long long)keep[h] * g.NB;
+  }
+  if (total >= (1ll << 31) || (long long)prob->n_heads * g.NB >= (1ll << 31) - 1) return PSA_ERR_UNSUPPORTED;
+  if (col_capacity < total) return PSA_ERR_CAPACITY;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  std::lock_guard<std::mutex> lock(g_mu);
+  long long base = 0;
+  for (int head0 = 0; head0 < prob->n_heads; head0 += kMaxHeads) {
+    const int n_here = prob->n_heads - head0 < kMaxHeads ? prob->n_heads - head0 : kMaxHeads;
+    const long long off = (long long)head0 * prob->stride_head;
+    SelectHeads heads;
+    for (int h = 0; h < n_here; ++h) {
+      heads.keep[h] = keep[head0 + h];
+      heads.base[h] = (int)base;
+      base += (long long)keep[head0 + h] * g.NB;
+    }
+    int launches = 0;
+    const cudaError_t e = launch_select(static_cast<const uint16_t*>(q) + off, static_cast<const uint16_t*>(k) + off, g, prob->stride_head, prob->stride_token,
+                                        heads, n_here, keep_self != 0, static_cast<double*>(scratch), row_ptr + (long long)head0 * g.NB, col_idx, st, &launches);
+    g_launches += launches;
+    if (e != cudaSuccess) return PSA_ERR_CUDA;
+  }
+  return PSA_OK;
+}
+
+static int lists_geom(const psa_problem* prob, int64_t n_text, int T, int H, int W, HostGeom* g) {
+  const int rc = make_geom(prob, T, H, W, true, g);
+  return rc != PSA_OK ? rc : set_text(g, n_text);
+}
+constexpr size_t kListsItemsOff = 256;   // of the scratch; the scheduler ticket is in front
+
+int64_t psa_attn_fwd_lists_scratch_bytes(const psa_problem* prob, int64_t n_text, int T, int H, int W) {
+  HostGeom g;
+  const int rc = lists_geom(prob, n_text, T, H, W, &g);
+  if (rc != PSA_OK) return rc;
+  return (int64_t)(kListsItemsOff + sizeof(WorkItem) * (size_t)(prob->n_heads < kMaxHeads ? prob->n_heads : kMaxHeads) * g.items_per_head);
+}
+
+int psa_attn_fwd_lists(const void* q, const void* k, const void* v, void* out, float* lse, const int32_t* row_ptr, const int32_t* col_idx,
+                       int64_t n_entries, const psa_problem* prob, int64_t n_text, int T, int H, int W, void* scratch, void* stream) {
+  HostGeom g;
+  int rc = lists_geom(prob, n_text, T, H, W, &g);
+  if (rc != PSA_OK) return rc;
+  if (!q || !k || !v || !out || !lse || !row_ptr || !scratch || n_entries < 0 || (n_entries > 0 && !col_idx)) return PSA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(scratch) || (reinterpret_cast<uintptr_t>(lse) & 3u) ||
+      (reinterpret_cast<uintptr_t>(row_ptr) & 3u) || (reinterpret_cast<uintptr_t>(col_idx) & 3u))
+    return PSA_ERR_INVALID_ARG;
+  if (out == q || out == k || out == v) return PSA_ERR_INVALID_ARG;
+  if (prob->stride_token < kHeadDim || (prob->stride_token % 8) != 0) return PSA_ERR_INVALID_ARG;
+  if (prob->n_heads > 1 && (prob->stride_head < kHeadDim || (prob->stride_head % 8) != 0)) return PSA_ERR_INVALID_ARG;
+  if (n_entries >= (1ll << 31) || (long long)prob->n_heads * g.NB >= (1ll << 31) - 1) return PSA_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  std::lock_guard<std::mutex> lock(g_mu);
+  int dev;
+  Workspace* ws;
+  int* status;
+  if ((rc = device_info(&dev, &ws)) != PSA_OK || (rc = init_attn(ws)) != PSA_OK || (rc = lists_status(dev, &status)) != PSA_OK) return rc;
+  // The lists' lengths are in device memory: an average row is taken for the choice of CTAs per item.
+  const std::vector<long long> weights((size_t)prob->n_heads, n_entries / prob->n_heads);
+  const int cluster = share_items(*ws, g, weights.data(), prob->n_heads).cluster;
+  ws->last_call = next_call_id(st);
+  ws->last_lists = true;
+  const Layout lay = {prob->stride_head, prob->stride_token, prob->stride_head, prob->stride_token, false};
+  for (int head0 = 0; head0 < prob->n_heads; head0 += kMaxHeads) {
+    const int n_here = prob->n_heads - head0 < kMaxHeads ? prob->n_heads - head0 : kMaxHeads;
+    const long long off = (long long)head0 * prob->stride_head;
+    TensorMapsCut all;
+    if ((rc = encode_maps(&all, static_cast<const uint16_t*>(q) + off, static_cast<const uint16_t*>(k) + off, static_cast<const uint16_t*>(v) + off,
+                          static_cast<uint16_t*>(out) + off, g, lay, n_here)) != PSA_OK)
+      return rc;
+    TensorMaps tm;
+    for (int i = 0; i < 3; ++i) {
+      tm.q[i] = all.q[i]; tm.k[i] = all.k[i]; tm.v[i] = all.v[i]; tm.o[i] = all.o[i];
+    }
+    AttnParamsLists prm;
+    static_cast<AttnParams&>(prm) = AttnParams{g, reinterpret_cast<const WorkItem*>(static_cast<char*>(scratch) + kListsItemsOff), nullptr, status,
+                                               lse + (long long)head0 * g.Lt, n_here * g.items_per_head, ws->last_call, 0,
+                                               static_cast<uint16_t*>(out) + off, prob->stride_head, prob->stride_token};
+    prm.g.n_heads = n_here;
+    prm.lists = KeyLists{row_ptr + (long long)head0 * g.NB, col_idx, (int)n_entries};
+    prm.counter = static_cast<int*>(scratch);
+    // items shared by CTAs are taken in order, whatever their number
+    const bool direct = cluster > 1 || runs_at_once(*ws, prm.n_items, cluster);
+    if (launch_lists(tm, prm, g, *ws, cluster, direct, st) != cudaSuccess) return PSA_ERR_CUDA;
+  }
+  return PSA_OK;
 }
 
 int psa_search_select_at_sparsity(const float* losses, const float* sparsity, int n, float target) {
@@ -1455,6 +1612,7 @@ int psa_selftest_wait_timeout(int limit_ms, void* stream) {
   if (rc != PSA_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ws->last_call = next_call_id(st);
+  ws->last_lists = false;
   if (launch_wait_probe(static_cast<int*>(ws->base), ws->last_call, 1000000ull * (unsigned long long)limit_ms, st) != cudaSuccess)
     return PSA_ERR_CUDA;
   ++g_launches;
@@ -1469,8 +1627,14 @@ int psa_last_device_status(int32_t* detail) {
   if (rc != PSA_OK) return rc;
   if (cudaDeviceSynchronize() != cudaSuccess) return PSA_ERR_CUDA;
   if (detail) *detail = 0;
-  if (!ws->base) return PSA_OK;
-  return read_status(ws->base, ws->last_call, detail);
+  // the words that the last call reports to, and the others for replays of captured calls (no call has id 0)
+  for (int last = 1; last >= 0; --last) {
+    void* header = (last == 1) == ws->last_lists ? (void*)g_lists_status_ptr[dev] : ws->base;
+    if (!header) continue;
+    rc = read_status(header, last == 1 ? ws->last_call : 0, detail);
+    if (rc != PSA_OK) return rc;
+  }
+  return PSA_OK;
 }
 
 int psa_shutdown(void) {
