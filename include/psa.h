@@ -247,7 +247,7 @@ int psa_search_select_at_sparsity(const float* losses, const float* sparsity, in
  *   the first dim_t / 2 pairs of channels turn with the token's frame, the next dim_h / 2 with its row, the next dim_w / 2 with
  *   its column, channels beyond dim_t + dim_h + dim_w = R not at all.  Pair j of an axis of d channels turns by
  *   (origin + step * index) * theta^(-2 j / d), computed in 64 bits.  Pair p is channels 2p and 2p + 1, or p and p + R / 2
- *   (PSA_PAIRS_HALVES; R a multiple of 8):  (a, b) -> (a cos - b sin, a sin + b cos).
+ *   (PSA_PAIRS_HALVES; R a multiple of 16):  (a, b) -> (a cos - b sin, a sin + b cos).
  * Tokens T*H*W .. T*H*W + n_text - 1 of the sequence (text) are normed and not rotated.  The tensors hold tokens first_token ..
  * first_token + n_tokens - 1 of the sequence, e.g. one rank's part (n_tokens 0: nothing happens).  Arithmetic in 32 bits, one
  * rounding at the end.
@@ -282,7 +282,7 @@ typedef struct {
   int32_t dim_t, dim_h, dim_w;          /* even, >= 0, sum <= 128 */
   int32_t pairs;                        /* psa_pairs              */
   double  theta;                        /* > 0                    */
-  double  origin[3], step[3];           /* frame, row, column     */
+  double  origin[3], step[3];           /* frame, row, column; the grid's largest angle below 2^48 quarter turns */
 } psa_rope;
 int psa_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, const void* q_weight, const void* k_weight,
                      const psa_qk* prob, const psa_rope* rope, int T, int H, int W, void* stream);

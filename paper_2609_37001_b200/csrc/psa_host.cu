@@ -1488,18 +1488,24 @@ static int norm_rope_args(const psa_qk* prob, const psa_rope* rope, int T, int H
     if (d < 0 || d > kHeadDim || (d & 1)) return PSA_ERR_INVALID_ARG;
   const int rotated = dims[0] + dims[1] + dims[2];
   if (rotated > kHeadDim || (rope->pairs != PSA_PAIRS_INTERLEAVED && rope->pairs != PSA_PAIRS_HALVES)) return PSA_ERR_INVALID_ARG;
-  if (rope->pairs == PSA_PAIRS_HALVES && rotated % 8 != 0) return PSA_ERR_UNSUPPORTED;
+  if (rope->pairs == PSA_PAIRS_HALVES && rotated % 16 != 0) return PSA_ERR_UNSUPPORTED;
   if (!(rope->theta > 0.0) || !std::isfinite(rope->theta)) return PSA_ERR_INVALID_ARG;
   std::memset(a, 0, sizeof(*a));
   for (int x = 0, p = 0; x < 3; ++x) {
-    if (!std::isfinite(rope->origin[x]) || !std::isfinite(rope->step[x])) return PSA_ERR_INVALID_ARG;
+    // (angles of the grid's positions, in quarter turns, are below 2^48: beyond that 64 bits have too little of a turn left)
+    const double last = std::fabs(rope->origin[x]) + std::fabs(rope->step[x]) * (x == 0 ? T : (x == 1 ? H : W));
+    const double fastest = dims[x] ? std::fmax(1.0, std::pow(rope->theta, 2.0 / dims[x] - 1.0)) : 0.0;   // (a theta below 1 makes later pairs faster)
+    if (!std::isfinite(rope->origin[x]) || !std::isfinite(rope->step[x]) || !(last * fastest < 281474976710656.0)) return PSA_ERR_INVALID_ARG;
     a->origin[x] = rope->origin[x];
     a->step[x] = rope->step[x];
-    for (int j = 0; j < dims[x] / 2; ++j) a->turns[p++] = std::pow(rope->theta, -2.0 * j / dims[x]) / 6.283185307179586476925;
+    for (int j = 0; j < dims[x] / 2; ++j) a->turns[p++] = std::pow(rope->theta, -2.0 * j / dims[x]) / 1.570796326794896619231;
     a->pairs[x] = p;
   }
   a->H = H;
   a->W = W;
+  a->by_h = divisor_of(H);
+  a->by_w = divisor_of(W);
+  a->by_tokens = divisor_of(prob->n_tokens > 0 ? (int)prob->n_tokens : 1);
   a->n_video = L;
   a->first_token = prob->first_token;
   a->n_tokens = (int)prob->n_tokens;

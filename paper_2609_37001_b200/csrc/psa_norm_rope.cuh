@@ -4,17 +4,30 @@
 
 namespace psa {
 
-constexpr int kNormRopeBwdBlocks = 296;   // most blocks a tensor in a gradient launch, each with a partial sum per weight
+constexpr int kNormRopeBwdBlocks = 444;   // most blocks a tensor in a gradient launch, each with a partial sum per weight
+
+// Division of numbers below 2^31 by a constant d: a shift for powers of two (m == 0), else the high half of a product, shifted.
+struct Divisor {
+  uint32_t m;
+  int shift;
+};
+inline Divisor divisor_of(int d) {
+  int l = 0;
+  while ((1ll << l) < d) ++l;
+  if ((1ll << l) == d) return Divisor{0u, l};
+  return Divisor{(uint32_t)((1ull << (31 + l)) / (unsigned)d + 1), l - 1};   // n < 2^31: exact, as m d - 2^(31 + l) <= d <= 2^l
+}
 
 struct NormRopeArgs {
-  double turns[64];                 // turns per unit of position of every pair, axis after axis
+  double turns[64];                 // quarter turns per unit of position of every pair, axis after axis
+  Divisor by_tokens, by_w, by_h;
   double origin[3], step[3];        // positions: origin + step * index
   int pairs[3];                     // pairs of the first axis, of the first two, of all three
   int H, W;
   long long n_video;                // tokens of the sequence that are rotated: T * H * W
   long long first_token;            // of the sequence
   int n_tokens, n_all, n_heads;     // tokens of a batch element, of all of them
-  int parts, slots;                 // half warps of a token; tokens of a block
+  int parts, slots, rows, sets;     // groups of a token; tokens of a block; rows (heads) of a group; sets of tokens in shared memory
   int weight_dtype, weight_head;    // weight_head: 1 if every head has weights of its own
   int weight_cols;                  // weights
   float eps, inv_count;             // inv_count: 1 / values of a mean
@@ -26,7 +39,7 @@ struct NormRopeArgs {
   long long in_batch, in_head, in_token, out_batch, out_head, out_token, dx_batch, dx_head, dx_token;   // strides, in elements
 };
 
-// Launches the forward pass or the gradient.  The arguments have been checked; parts and slots are chosen here.
+// Launches the forward pass or the gradient.  The arguments have been checked; parts, slots, rows and sets are chosen here.
 cudaError_t launch_norm_rope(NormRopeArgs& a, const psa_qk& prob, bool halves, bool backward, int n_sms, float* q_dw, float* k_dw, cudaStream_t st,
                              int* launches);
 
