@@ -5,19 +5,22 @@
 // every pair of channels; the mean goes over the head's channels or over those of all heads of the token.  The gradient:
 // g = R(-angles) dy, h = w * g, s = mean(h * x):  dx = r * (h - x * r^2 * s),  dw = sum of g * x * r.
 //
-// Bound by HBM: forward moves each value in and out once, the gradient x and dy in and dx out.  A group of eight lanes takes
-// up to kRows rows (heads) of one token, 16 channels a lane; several groups share a token.  Blocks are persistent, and every
-// thread copies what it needs of the block's next token into shared memory (cp.async) while it works on this one: loads are
-// always in flight without holding registers, a second look at a row (the mean over all heads) costs no second read, and no
-// thread waits for another's copies.  The next bound is the issue of instructions (some 100 a row in a first version that
-// held rows in registers, 65 % of the issue slots at 44 % of HBM): eight lanes a row instead of 16 halve what is spent on addresses,
-// sums over lanes and roots, arithmetic runs on packed pairs of 32-bit values, and cos and sin of a token's 64 pairs are computed
-// once for all its rows of q and k, into shared memory, while the token before is worked on.
+// Bound by HBM: forward moves each value in and out once, the gradient x and dy in and dx out.  A group of eight lanes takes one
+// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64); a block takes one or more tokens of
+// q and k, or (more than 16 heads) of one of them, all heads, so that a mean over all heads costs one read.  Blocks are persistent: a group's head is always the same, whose
+// weights, and sums for dw, stay in registers.  Two more warps of the block, the producers, copy the next tokens' rows into shared
+// memory (cp.async, kMaxStages sets at most) and compute cos and sin of their 64 pairs, once for all heads.
+// The next bound is the issue of instructions (some 100 a row in a first version where every thread loaded its own rows and
+// computed its own angles, 65 % of the issue slots at 44 % of HBM): what is done for a token and not for a channel is left to the
+// producers, eight lanes a row instead of 16 halve what is spent on addresses, sums over lanes and roots, and arithmetic runs on
+// packed pairs of 32-bit values.
 //
 // Angles: position times frequency in 64 bits, as only the fraction of a turn counts and positions may be far; the distance
 // to the nearest quarter turn then in 32 bits.  Sums, norms and rotations are in 32 bits, rounded once.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "psa_norm_rope.cuh"
 
@@ -25,10 +28,19 @@ namespace psa {
 
 namespace {
 
-constexpr int kRows = 2;          // rows (heads) of a token that one group takes (more than 64 heads: twice as many going forward)
 constexpr int kLanes = 8;         // lanes of a group
 constexpr int kPairs = kHeadDim / 2;
-constexpr int kMaxThreads = 256;  // forward; backward twice as many (kMaxHeads / kRows groups)
+constexpr int kMaxThreads = 512;   // besides the producers
+constexpr int kProducers = 64;     // threads: one a pair
+constexpr int kMaxStages = 4;      // sets of rows in shared memory
+constexpr int kMaxGroups = kMaxThreads / kLanes;
+// Registers.  Forward 80, which are 24 warps an SM: with 64, 72 and 88, 24 heads of 115,456 tokens took 595, 559 and 587 us instead of
+// 520.  The gradient's sums, weights, x and dy want 104: 40 heads of 75,600 tokens with the norm over all heads take 1.01 ms as one
+// block an SM, and 1.17 with 80 registers and two.  (96 where a block of kMaxThreads + kProducers threads has to start.)
+constexpr int kRegs = 80, kBwdRegs = 104;
+// Threads of a block besides the producers, at most: with q and k, with several tokens.  (The producers are kept as busy by one
+// token as by one of few heads.)
+constexpr int kBlockThreads = 256, kSmallThreads = 64;
 
 // ------------------------------------------------------------------------------------------------ packed pairs
 typedef unsigned long long f2;    // two fp32 values, one instruction for both
@@ -52,7 +64,6 @@ __device__ __forceinline__ f2 mul(f2 a, f2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ f2 negate(f2 a) { return a ^ 0x8000000080000000ull; }
 __device__ __forceinline__ float sum(f2 a) {
   const float2 v = unpack(a);
   return v.x + v.y;
@@ -79,30 +90,19 @@ __device__ __forceinline__ void load_row(const T* p, int c0, int c1, Raw<T>& r) 
     *reinterpret_cast<uint4*>(r.w + 4 * (kVec + i)) = reinterpret_cast<const uint4*>(p + c1)[i];
   }
 }
-// The same by way of shared memory: word i of a thread lies at i * blockDim words of 16 bytes from its first, where only this thread
-// writes and reads.
-template <class T>
-__device__ __forceinline__ void copy_row(uint32_t to, const T* p, int c0, int c1) {
-  constexpr int kVec = sizeof(T) / 2;
-  const uint32_t step = blockDim.x * 16u;
-#pragma unroll
-  for (int i = 0; i < 2 * kVec; ++i)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * step), "l"(p + (i < kVec ? c0 : c1) + (i % kVec) * (16 / (int)sizeof(T))) : "memory");
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLater>   // all but the last kLater sets of copies have arrived
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLater) : "memory"); }
-// Zeros in all of a thread's words, for the rows that it has no head for.
-__device__ __forceinline__ void clear_rows(uint4* rows, int words) {
-  for (int i = 0; i < words; ++i) rows[i * blockDim.x] = make_uint4(0u, 0u, 0u, 0u);
+// All but the last `later` sets of copies have arrived.
+__device__ __forceinline__ void copies_wait(int later) {
+  if (later >= 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (later == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
-template <class T>
-__device__ __forceinline__ Raw<T> read_row(const uint4* from) {
-  Raw<T> r;
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T); ++i) *reinterpret_cast<uint4*>(r.w + 4 * i) = from[i * blockDim.x];
-  return r;
-}
+// Of all threads; of all but the producers.
+__device__ __forceinline__ void consumer_barrier() { asm volatile("bar.sync 1, %0;" ::"r"(blockDim.x - kProducers) : "memory"); }
+__device__ __forceinline__ void block_barrier() { asm volatile("bar.sync 0;" ::: "memory"); }
 __device__ __forceinline__ float2 pair_of(uint32_t w, const __nv_bfloat16*) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ float2 pair_of(uint32_t w, const __half*) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 template <class T, bool kHalves>
@@ -232,7 +232,8 @@ __device__ __forceinline__ float lanes_sum2(float x, float y) {
 // A lane's place: which channels of a row it holds, and which group of which token of the block it belongs to.
 struct Place {
   int c0, c1;          // its two runs of eight channels
-  int slot, part;      // token of the block, group of that token
+  int set, part;       // token and tensor of the block, group of that one
+  int slot, t;         // token of the block; tensor
   bool idle;           // beyond the last group of the last token
 };
 template <bool kHalves>
@@ -248,10 +249,12 @@ __device__ __forceinline__ Place place_of(const NormRopeArgs& a) {
     p.c0 = 8 * lane;
     p.c1 = p.c0 + 64;
   }
-  p.slot = group / a.parts;
-  p.part = group - p.slot * a.parts;
-  p.idle = p.slot >= a.slots;
-  if (p.idle) p.slot = p.part = 0;   // (it looks at a token's turns like the others)
+  p.set = group / a.parts;
+  p.part = group - p.set * a.parts;
+  p.idle = p.set >= a.slots * a.tensors;
+  if (p.idle) p.set = p.part = 0;   // (it looks at a token's turns like the others)
+  p.slot = a.tensors == 2 ? p.set >> 1 : p.set;
+  p.t = a.tensors == 2 ? p.set & 1 : (int)blockIdx.y;
   return p;
 }
 
@@ -281,21 +284,28 @@ __device__ __forceinline__ void quarter_turn(float x, float& c, float& s) {
   c = fmaf(t2, q, 1.f);
 }
 
-// cos and sin of the 64 pairs of the block's tokens from `first` on into shared memory, [token][cos 64, sin 64]; 1 and 0 where nothing
-// turns.  angles: quarter turns of every pair, {per index, at index 0}.
-__device__ __forceinline__ void fill_turns(const NormRopeArgs& a, const double2* angles, int first, float* turns) {
-  for (int e = (int)threadIdx.x; e < a.slots * kPairs; e += (int)blockDim.x) {
-    const int slot = e / kPairs, p = e % kPairs, n = first + slot;
-    if (n >= a.n_all || n < 0) continue;
+// A pair's quarter turns: per index of its axis, and at index 0.
+struct Angle {
+  int axis;            // 3: it does not turn
+  double per, at0;
+};
+__device__ __forceinline__ Angle angle_of(const NormRopeArgs& a, int p) {
+  const int axis = p < a.pairs[0] ? 0 : (p < a.pairs[1] ? 1 : (p < a.pairs[2] ? 2 : 3));
+  return Angle{axis, axis < 3 ? a.step[axis] * a.turns[p] : 0.0, axis < 3 ? a.origin[axis] * a.turns[p] : 0.0};
+}
+// cos, sin and -sin of pair p of the block's tokens from `first` on into shared memory, [token][3][64]; 1 and 0 where nothing turns.
+__device__ __forceinline__ void fill_turns(const NormRopeArgs& a, const Angle& angle, int p, int first, float* turns) {
+  for (int slot = 0; slot < a.slots; ++slot, turns += 3 * kPairs) {
+    const int n = first + slot;
+    if (n >= a.n_all || n < 0) break;
     int b, i;
     token_of(a, n, b, i);
     const long long at = a.first_token + i;
     float c = 1.f, s = 0.f;
-    if (p < a.pairs[2] && at < a.n_video) {
+    if (angle.axis < 3 && at < a.n_video) {
       const int j = (int)at, row = divide(j, a.by_w), t = divide(row, a.by_h);
-      const int index = p < a.pairs[0] ? t : (p < a.pairs[1] ? row - t * a.H : j - row * a.W);
-      const double2 angle = angles[p];
-      const double quarters = __fma_rn(angle.x, (double)index, angle.y);
+      const int index = angle.axis == 0 ? t : (angle.axis == 1 ? row - t * a.H : j - row * a.W);
+      const double quarters = __fma_rn(angle.per, (double)index, angle.at0);
       // the nearest whole number of quarters, in the last bits of the sum (the host bounds positions far below 2^51)
       const double shifted = quarters + 6755399441055744.0;   // 1.5 * 2^52
       const int q = __double2loint(shifted);
@@ -306,40 +316,54 @@ __device__ __forceinline__ void fill_turns(const NormRopeArgs& a, const double2*
       c = __uint_as_float(__float_as_uint(c) ^ (uint32_t)((q + 1) & 2) << 30);
       s = __uint_as_float(__float_as_uint(s) ^ (uint32_t)(q & 2) << 30);
     }
-    turns[slot * 2 * kPairs + p] = c;
-    turns[slot * 2 * kPairs + kPairs + p] = s;
+    turns[p] = c;
+    turns[kPairs + p] = s;
+    turns[2 * kPairs + p] = -s;
   }
 }
 
 // A lane's angles at its token, and which of its pairs turn (where none does a value that is not finite stays in its channel).
 struct Turn {
-  f2 c[4], s[4];
+  f2 c[4], s[4], m[4];   // cos, sin, -sin
   uint32_t some;
+  bool all;              // every pair of every lane of the warp turns
 };
-template <bool kHalves>
-__device__ __forceinline__ Turn turn_of(const NormRopeArgs& a, const float* from, bool video) {
+// turns: the token's; some: the lane's pairs that turn at video tokens.
+template <bool kHalves, bool kBack>
+__device__ __forceinline__ Turn turn_of(const float* turns, uint32_t some, bool video) {
   const int lane = (int)threadIdx.x & (kLanes - 1), p0 = (kHalves ? 8 : 4) * lane, p1 = kHalves ? p0 + 4 : p0 + 32;
-  const float4 c0 = *reinterpret_cast<const float4*>(from + p0), c1 = *reinterpret_cast<const float4*>(from + p1),
-               s0 = *reinterpret_cast<const float4*>(from + kPairs + p0), s1 = *reinterpret_cast<const float4*>(from + kPairs + p1);
   Turn t;
-  t.c[0] = pack(c0.x, c0.y); t.c[1] = pack(c0.z, c0.w); t.c[2] = pack(c1.x, c1.y); t.c[3] = pack(c1.z, c1.w);
-  t.s[0] = pack(s0.x, s0.y); t.s[1] = pack(s0.z, s0.w); t.s[2] = pack(s1.x, s1.y); t.s[3] = pack(s1.z, s1.w);
-  auto bits = [&](int from) -> uint32_t { return (1u << max(0, min(4, a.pairs[2] - from))) - 1u; };
-  t.some = video ? bits(p0) | bits(p1) << 4 : 0u;
+  f2* to[3] = {t.c, t.s, t.m};
+#pragma unroll
+  for (int k = 0; k < (kBack ? 2 : 3); ++k) {
+    const float4 x = *reinterpret_cast<const float4*>(turns + k * kPairs + p0), y = *reinterpret_cast<const float4*>(turns + k * kPairs + p1);
+    to[k][0] = pack(x.x, x.y); to[k][1] = pack(x.z, x.w); to[k][2] = pack(y.x, y.y); to[k][3] = pack(y.z, y.w);
+  }
+  if (kBack) {   // (registers are scarce there)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t.m[k] = t.s[k] ^ 0x8000000080000000ull;
+  }
+  t.some = video ? some : 0u;
+  t.all = __all_sync(0xffffffffu, t.some == 255u);
   return t;
 }
+template <bool kHalves>
+__device__ __forceinline__ uint32_t pairs_that_turn(const NormRopeArgs& a) {
+  const int lane = (int)threadIdx.x & (kLanes - 1), p0 = (kHalves ? 8 : 4) * lane, p1 = kHalves ? p0 + 4 : p0 + 32;
+  auto bits = [&](int from) -> uint32_t { return (1u << max(0, min(4, a.pairs[2] - from))) - 1u; };
+  return bits(p0) | bits(p1) << 4;
+}
 
-// Rotates the lane's pairs, by the opposite angles for kBack.  all: every pair of every lane of the warp turns.
+// Rotates the lane's pairs, by the opposite angles for kBack.
 template <bool kBack>
-__device__ __forceinline__ Row rotate(const Turn& t, bool all, const Row& x) {
+__device__ __forceinline__ Row rotate(const Turn& t, const Row& x) {
   Row y;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const f2 sa = kBack ? t.s[k] : negate(t.s[k]), sb = kBack ? negate(t.s[k]) : t.s[k];
-    y.a[k] = fma(x.b[k], sa, mul(x.a[k], t.c[k]));
-    y.b[k] = fma(x.a[k], sb, mul(x.b[k], t.c[k]));
+    y.a[k] = fma(x.b[k], kBack ? t.s[k] : t.m[k], mul(x.a[k], t.c[k]));
+    y.b[k] = fma(x.a[k], kBack ? t.m[k] : t.s[k], mul(x.b[k], t.c[k]));
   }
-  if (!all) {
+  if (!t.all) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const bool lo = (t.some >> (2 * k)) & 1u, hi = (t.some >> (2 * k + 1)) & 1u;
@@ -351,320 +375,302 @@ __device__ __forceinline__ Row rotate(const Turn& t, bool all, const Row& x) {
   return y;
 }
 
-// Sum over the groups of a token, which every one of them gets; all threads of the block.  `buf`: one float a group, not
-// written again before the next barrier.
-__device__ __forceinline__ float token_sum(const NormRopeArgs& a, const Place& p, const float* buf) {
-  const int lane = (int)threadIdx.x & (kLanes - 1);
-  float x = 0.f;
-  if (!p.idle)
-    for (int j = lane; j < a.parts; j += kLanes) x += buf[p.slot * a.parts + j];
-  return lanes_sum(x);
+// Sums (of two values) over the groups of a token's tensor, which every one of them gets.  `sums`: the token's, one entry a group.
+__device__ __forceinline__ float2 token_sum(const float2* sums, int parts) {
+  float2 v = make_float2(0.f, 0.f);
+#pragma unroll 4
+  for (int j = (int)threadIdx.x & (kLanes - 1); j < parts; j += kLanes) {
+    const float2 x = sums[j];
+    v.x += x.x;
+    v.y += x.y;
+  }
+  return make_float2(lanes_sum(v.x), lanes_sum(v.y));
+}
+__device__ __forceinline__ float token_sum(const float* sums, int parts) {
+  float v = 0.f;
+#pragma unroll 4
+  for (int j = (int)threadIdx.x & (kLanes - 1); j < parts; j += kLanes) v += sums[j];
+  return lanes_sum(v);
 }
 
-// Shared memory: frequencies, shared weights, the turns of two sets of tokens, sums of the groups, the rows of two sets of tokens.
+// Shared memory: the turns of two sets of tokens, sums of the groups, the sets of rows ([token][head], x and then dy).
 struct Shared {
-  double2* angles; // [64]
-  float* weights;  // [2][128]
-  float* turns;    // [2][tokens][cos 64, sin 64]
-  float* sums;     // [2][2][groups]
-  uint4* rows;     // [sets][words of a thread][threads], from this thread's on
+  float* turns;      // [2][tokens][cos, sin, -sin][64]
+  float2* sums;      // [2][groups]
+  uint8_t* rows;
 };
-__device__ __forceinline__ Shared carve(const NormRopeArgs& a, double* sm) {
-  float* f = reinterpret_cast<float*>(sm + 2 * kPairs) + 2 * kHeadDim;
-  const int n = a.slots * 2 * kPairs, groups = (int)blockDim.x / kLanes;
-  return Shared{reinterpret_cast<double2*>(sm), f - 2 * kHeadDim, f, f + 2 * n, reinterpret_cast<uint4*>(f + 2 * n + 4 * groups) + threadIdx.x};
+__device__ __forceinline__ Shared carve(const NormRopeArgs& a, uint8_t* sm) {
+  float* turns = reinterpret_cast<float*>(sm);
+  float2* sums = reinterpret_cast<float2*>(turns + 6 * a.slots * kPairs);
+  return Shared{turns, sums, reinterpret_cast<uint8_t*>(sums + 2 * kMaxGroups)};
 }
-// What a block keeps: the pairs' angles, and weights that all heads share (of tensors t0 .. t1 - 1).
-template <bool kHasNorm>
-__device__ __forceinline__ void fill_constants(const NormRopeArgs& a, const Shared& sh, int t0, int t1) {
-  for (int i = (int)threadIdx.x; i < kPairs; i += (int)blockDim.x) {
-    const int axis = i < a.pairs[0] ? 0 : (i < a.pairs[1] ? 1 : 2);
-    sh.angles[i] = make_double2(a.step[axis] * a.turns[i], a.origin[axis] * a.turns[i]);
-  }
-  if (kHasNorm && a.weight_head == 0) {
-    for (int i = (int)threadIdx.x; i < (t1 - t0) * kHeadDim; i += (int)blockDim.x) {
-      const int t = t0 + i / kHeadDim, c = i % kHeadDim;
-      const void* w = a.weight[t];
-      sh.weights[t * kHeadDim + c] = w == nullptr ? 1.f
-                                     : a.weight_dtype == PSA_FP32 ? static_cast<const float*>(w)[c]
-                                     : a.weight_dtype == PSA_FP16 ? __half2float(static_cast<const __half*>(w)[c])
-                                                                  : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c]);
-    }
-  }
+// bytes: of the rows of a set of tokens
+constexpr size_t shared_bytes(int slots, int bytes, int stages) {
+  return (size_t)6 * slots * kPairs * sizeof(float) + 2 * kMaxGroups * sizeof(float2) + (size_t)stages * bytes;
 }
-// words: of 16 bytes, of a thread and one set of tokens.  Where two sets do not fit (more than 110 heads of fp32) there is one, which is
-// copied when the tokens before have been worked on: 1; else 2.
-constexpr size_t shared_bytes(int slots, int threads, int words, int sets) {
-  return 2 * kPairs * sizeof(double) + 2 * kHeadDim * sizeof(float) + (size_t)(4 * slots * kPairs + 4 * (threads / kLanes)) * sizeof(float) + (size_t)sets * words * threads * 16;
-}
-int sets_of(int slots, int threads, int words) { return shared_bytes(slots, threads, words, 2) <= kMaxSmemBytes ? 2 : 1; }
 
-// ------------------------------------------------------------------------------------------------ forward
-template <class T, class O, int kNorm, bool kHalves>
-__global__ void __launch_bounds__(kMaxThreads, sizeof(T) == 4 ? 2 : 3)   // (80 registers: 24 warps an SM)
-norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
-  constexpr int kWords = sizeof(T);   // 16-byte words of a row and lane
-  extern __shared__ __align__(16) double sm[];
-  const Shared sh = carve(a, sm);
-  const Place p = place_of<kHalves>(a);
-  const int groups = (int)blockDim.x / kLanes, group = (int)threadIdx.x / kLanes, stride = (int)gridDim.x * a.slots;
-  const int tensors = a.in[1] != nullptr ? 2 : 1, per_group = a.rows;
-  const int row_step = kWords * (int)blockDim.x, tensor_step = per_group * row_step, set_step = 2 * tensor_step;   // in shared memory
-  const long long in_step = a.parts * a.in_head, out_step = a.parts * a.out_head;                                  // from a row to the next
-  const uint32_t rows_shared = (uint32_t)__cvta_generic_to_shared(sh.rows);
-  int first = (int)blockIdx.x * a.slots;   // token, batches behind one another
-  // rows of the group at token n: row u is there if u * parts is below
-  auto rows_of = [&](int n) -> int { return !p.idle && n < a.n_all && n >= 0 ? a.n_heads - p.part : 0; };
-  // the token copied last: its number, where its first row is and goes
-  int i = 0;
-  long long in_at = 0, out_at = 0;
-  const long long in_stride = stride * a.in_token, out_stride = stride * a.out_token;
-  const bool one_batch = a.n_all == a.n_tokens;
-  auto copy = [&](int n, int set, bool again) {
-    const int rows = rows_of(n);
-    if (again && one_batch) {
-      i += stride;
-      in_at += in_stride;
-      out_at += out_stride;
-    } else if (rows > 0) {
-      int b;
-      token_of(a, n, b, i);
-      in_at = b * a.in_batch + i * a.in_token + p.part * a.in_head;
-      out_at = b * a.out_batch + i * a.out_token + p.part * a.out_head;
-    }
-    const uint32_t to = rows_shared + (uint32_t)(set * set_step) * 16u;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (t == tensors) break;
-      const T* x = static_cast<const T*>(a.in[t]) + in_at;
-#pragma unroll
-      for (int u = 0; u < 2 * kRows; ++u, x += in_step) {
-        if (u == per_group) break;
-        if (u * a.parts < rows) copy_row(to + (uint32_t)(t * tensor_step + u * row_step) * 16u, x, p.c0, p.c1);
-      }
-    }
+// The producers' part: what lies in front of the first barrier, between two, and behind the last one.  Every block barrier of the
+// others has its like here: one a set of tokens in front of it, and (a single stage) one when it has been read.
+template <class T, class O>
+__device__ __forceinline__ void produce(const NormRopeArgs& a, const Shared& sh, bool x_too, bool g_too) {
+  const int me = (int)threadIdx.x - ((int)blockDim.x - kProducers), stride = (int)gridDim.x * a.slots;
+  const int x_bytes = x_too ? kHeadDim * (int)sizeof(T) : 0, token_bytes = a.n_heads * (x_bytes + (g_too ? kHeadDim * (int)sizeof(O) : 0));
+  const int stages = a.stages;
+  const uint32_t rows = (uint32_t)__cvta_generic_to_shared(sh.rows);
+  // 16-byte piece `me % pieces` of every (kProducers / pieces)-th head
+  auto copy_rows = [&](const auto* from, long long head_stride, uint32_t to) {
+    using E = typename std::remove_cv<typename std::remove_pointer<decltype(from)>::type>::type;
+    constexpr int kPieces = kHeadDim * (int)sizeof(E) / 16, kStep = kProducers / kPieces;
+    const int piece = me % kPieces, h0 = me / kPieces;
+    const E* p = from + h0 * head_stride + piece * (16 / (int)sizeof(E));
+    to += (uint32_t)(h0 * kHeadDim * (int)sizeof(E) + piece * 16);
+    const long long step = kStep * head_stride;
+#pragma unroll 4
+    for (int h = h0; h < a.n_heads; h += kStep, p += step, to += kStep * kHeadDim * sizeof(E)) copy16(to, p);
   };
-  if (per_group * a.parts != a.n_heads) clear_rows(sh.rows, a.sets * 2 * per_group * kWords);
-  copy(first + p.slot, 0, false);
-  copies_end();
-  fill_constants<kNorm != PSA_NORM_NONE>(a, sh, 0, tensors);
-  __syncthreads();
-  fill_turns(a, sh.angles, first, sh.turns);
+  auto issue = [&](int first, int stage) {
+    if (first < a.n_all) {
+      for (int slot = 0; slot < a.slots; ++slot) {
+        const int n = first + slot;
+        if (n >= a.n_all || n < 0) break;
+        int b, i;
+        token_of(a, n, b, i);
+        for (int k = 0; k < a.tensors; ++k) {
+          const int t = a.tensors == 2 ? k : (int)blockIdx.y;
+          const uint32_t to = rows + (uint32_t)(((stage * a.slots + slot) * a.tensors + k) * token_bytes);
+          if (x_too) copy_rows(static_cast<const T*>(a.in[t]) + (b * a.in_batch + i * a.in_token), a.in_head, to);
+          if (g_too) copy_rows(static_cast<const O*>(a.grad[t]) + (b * a.out_batch + i * a.out_token), a.out_head, to + (uint32_t)(a.n_heads * x_bytes));
+        }
+      }
+    }
+    copies_end();
+  };
+  // first tokens of the sets to be copied, and computed with; a sum that passes 2^31 is the end, too
+  auto after = [&](int first) -> int { return a.n_all - first > stride ? first + stride : a.n_all; };
+  const Angle angle = angle_of(a, me);
+  int first = (int)blockIdx.x * a.slots, ahead = first, stage = 0;
+  const int depth = stages > 1 ? stages - 1 : 1;   // sets in flight
+  for (int k = 0; k < depth; ++k, ahead = after(ahead)) issue(ahead, k);
+  fill_turns(a, angle, me, first, sh.turns);
+  copies_wait(depth - 1);
   for (int it = 0; first < a.n_all; ++it) {
-    const int next = a.n_all - first > stride ? first + stride : a.n_all, rows = rows_of(first + p.slot);
-    const int i_here = i;
-    const long long out_here = out_at;
-    const uint4* mine = sh.rows;
-    if (a.sets == 2) {
-      if (next < a.n_all) copy(next + p.slot, (it + 1) & 1, true);
-      copies_end();
-      copies_wait<1>();
-      mine += (it & 1) * set_step;
+    block_barrier();   // set `it` is there, and nobody reads the one before any more
+    const int next = after(first);
+    float* turns = sh.turns + ((it + 1) & 1) * 3 * a.slots * kPairs;
+    if (stages > 1) {
+      issue(ahead, stage == 0 ? stages - 1 : stage - 1);
+      ahead = after(ahead);
+      stage = stage + 1 == stages ? 0 : stage + 1;
+      if (next < a.n_all) fill_turns(a, angle, me, next, turns);
+      copies_wait(depth - 1);
     } else {
-      copies_wait<0>();
-    }
-    float* sums = sh.sums + (it & 1) * 2 * groups;
-    if constexpr (kNorm == PSA_NORM_TOKEN) {
-      float ss[2] = {0.f, 0.f};
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t == tensors) break;
-        for (int u = 0; u < per_group; ++u) {
-          const Row x = row_of<T, kHalves>(read_row<T>(mine + t * tensor_step + u * row_step));
-          ss[t] += dot(x, x);
-        }
-      }
-      const float s = lanes_sum2(ss[0], ss[1]);
-      if ((threadIdx.x & 3) == 0) sums[((threadIdx.x >> 2) & 1) * groups + group] = s;
-    }
-    __syncthreads();
-    if (next < a.n_all) fill_turns(a, sh.angles, next, sh.turns + ((it + 1) & 1) * a.slots * 2 * kPairs);
-    const Turn turn = turn_of<kHalves>(a, sh.turns + ((it & 1) * a.slots + p.slot) * 2 * kPairs, a.first_token + i_here < a.n_video);
-    const bool all = __all_sync(0xffffffffu, turn.some == 255u);
-#pragma unroll 1
-    for (int t = 0; t < tensors; ++t) {
-      float r = 1.f;
-      if constexpr (kNorm == PSA_NORM_TOKEN) r = rsqrtf(token_sum(a, p, sums + t * groups) * a.inv_count + a.eps);
-      O* to = static_cast<O*>(a.out[t]) + out_here;
-      const uint4* from = mine + t * tensor_step;
-      Row w;
-      if (kNorm != PSA_NORM_NONE && a.weight_head == 0) w = weight_of<float, kHalves>(sh.weights, t * kHeadDim, p.c0, p.c1);
-#pragma unroll 1
-      for (int u = 0; u < per_group; ++u, from += row_step, to += out_step) {
-        Row x = row_of<T, kHalves>(read_row<T>(from));
-        if constexpr (kNorm == PSA_NORM_HEAD) r = rsqrtf(lanes_sum(dot(x, x)) * a.inv_count + a.eps);
-        if (u * a.parts >= rows) continue;
-        if constexpr (kNorm != PSA_NORM_NONE) {
-          if (a.weight_head != 0) w = load_weight<kHalves>(a.weight[t], a.weight_dtype, (p.part + u * a.parts) * kHeadDim, p.c0, p.c1);
-          x = times(times(x, w), r);
-        }
-        store_row<O, kHalves>(to, p.c0, p.c1, rotate<false>(turn, all, x));
-      }
-    }
-    if (a.sets == 1 && next < a.n_all) {
-      copy(next + p.slot, 0, true);
-      copies_end();
+      block_barrier();   // set `it` has been read
+      issue(ahead, 0);
+      ahead = after(ahead);
+      if (next < a.n_all) fill_turns(a, angle, me, next, turns);
+      copies_wait(0);
     }
     first = next;
+  }
+  copies_wait(0);
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+template <class T, class O, int kNorm, bool kHalves, int kRows>
+__global__ void __maxnreg__(kRows == 1 ? kRegs : 96)
+norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
+  extern __shared__ __align__(16) uint8_t sm[];
+  const Shared sh = carve(a, sm);
+  if (threadIdx.x >= blockDim.x - kProducers) {
+    produce<T, O>(a, sh, true, false);
+    return;
+  }
+  const Place p = place_of<kHalves>(a);
+  const int t = p.t, group = (int)threadIdx.x / kLanes, stride = (int)gridDim.x * a.slots;
+  const uint32_t some = pairs_that_turn<kHalves>(a);
+  Row w[kRows];
+  if constexpr (kNorm != PSA_NORM_NONE) {
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+      w[u] = load_weight<kHalves>(a.weight[t], a.weight_dtype, a.weight_head ? min(p.part + u * a.parts, a.n_heads - 1) * kHeadDim : 0, p.c0, p.c1);
+  }
+  int n = (int)blockIdx.x * a.slots + p.slot, i = 0;   // token, batches behind one another; within its batch element
+  O* to = static_cast<O*>(a.out[t]);                    // where its first row goes
+  auto there = [&](int u) -> bool { return !p.idle && n < a.n_all && n >= 0 && (kRows == 1 || p.part + u * a.parts < a.n_heads); };
+  if (there(0)) {
+    int b;
+    token_of(a, n, b, i);
+    to += b * a.out_batch + i * a.out_token + p.part * a.out_head;
+  }
+  const int over = stride / a.n_tokens, step = stride - over * a.n_tokens;   // to the block's next tokens: batch elements, tokens
+  const long long to_step = over * a.out_batch + step * a.out_token;
+  const T* rows = reinterpret_cast<const T*>(sh.rows) + (p.set * a.n_heads + p.part) * kHeadDim;
+  const int set_step = a.slots * a.tensors * a.n_heads * kHeadDim;
+  int stage = 0;
+  for (int it = 0, first = (int)blockIdx.x * a.slots; first < a.n_all; ++it) {
+    block_barrier();
+    const Turn turn = turn_of<kHalves, false>(sh.turns + ((it & 1) * a.slots + p.slot) * 3 * kPairs, some, a.first_token + i < a.n_video);
+    Row x[kRows];
+    float ss[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      Raw<T> raw;
+      load_row(rows + stage * set_step + (kRows == 1 ? 0 : min(u * a.parts, a.n_heads - 1 - p.part) * kHeadDim), p.c0, p.c1, raw);
+      x[u] = row_of<T, kHalves>(raw);
+      if (kNorm != PSA_NORM_NONE) ss[u] = lanes_sum(dot(x[u], x[u]));
+    }
+    if constexpr (kNorm == PSA_NORM_TOKEN) {
+      float* sums = reinterpret_cast<float*>(sh.sums) + (it & 1) * kMaxGroups;
+      if ((threadIdx.x & (kLanes - 1)) == 0) sums[group] = kRows == 1 ? ss[0] : ss[0] + (p.part + a.parts < a.n_heads ? ss[kRows - 1] : 0.f);
+      consumer_barrier();
+      ss[0] = ss[kRows - 1] = token_sum(sums + p.set * a.parts, a.parts);
+    }
+    if (a.stages == 1) block_barrier();
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      if (!there(u)) continue;
+      if constexpr (kNorm != PSA_NORM_NONE) x[u] = times(times(x[u], w[u]), rsqrtf(ss[u] * a.inv_count + a.eps));
+      store_row<O, kHalves>(to + u * a.parts * a.out_head, p.c0, p.c1, rotate<false>(turn, x[u]));
+    }
+    first = a.n_all - first > stride ? first + stride : a.n_all;
+    n = first + p.slot;
+    i += step;
+    to += to_step;
+    if (i >= a.n_tokens) {
+      i -= a.n_tokens;
+      to += a.out_batch - a.n_tokens * a.out_token;
+    }
+    stage = stage + 1 == a.stages ? 0 : stage + 1;
   }
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// Like the forward pass, one tensor a block (blockIdx.y).  The sums for dw of a group's rows (kHeadWeights), or of all of them
-// together, stay in registers; every block leaves one partial sum per weight, which norm_rope_dw_kernel adds in a fixed order.
-template <class T, class O, int kNorm, bool kHalves, bool kHeadWeights>
-__global__ void __launch_bounds__(2 * kMaxThreads)
+// Like the forward pass.  Every block leaves one partial sum per weight, which norm_rope_dw_kernel adds in a fixed order.
+template <class T, class O, int kNorm, bool kHalves, int kRows>
+__global__ void __maxnreg__(kRows == 1 ? kBwdRegs : 96)
 norm_rope_bwd_kernel(const __grid_constant__ NormRopeArgs a) {
   constexpr bool kHasNorm = kNorm != PSA_NORM_NONE;
-  constexpr int kSums = kHeadWeights ? kRows : 1;
-  constexpr int kWords = kHasNorm ? sizeof(T) : 0, kGradWords = sizeof(O);   // 16-byte words of a row and lane
-  extern __shared__ __align__(16) double sm[];
+  extern __shared__ __align__(16) uint8_t sm[];
   const Shared sh = carve(a, sm);
+  const int consumers = (int)blockDim.x - kProducers;
+  float* dw_part = reinterpret_cast<float*>(sm);   // (at the end) [groups][128] of one row
+  Row dw[kRows];
   const Place p = place_of<kHalves>(a);
-  const int groups = (int)blockDim.x / kLanes, group = (int)threadIdx.x / kLanes, stride = (int)gridDim.x * a.slots, t = blockIdx.y;
-  const int per_group = a.rows, x_words = kWords * (int)blockDim.x, row_step = (kWords + kGradWords) * (int)blockDim.x, set_step = per_group * row_step;
-  const long long x_step = a.parts * a.in_head, g_step = a.parts * a.out_head, dx_step = a.parts * a.dx_head;   // from a row to the next
-  const uint32_t rows_shared = (uint32_t)__cvta_generic_to_shared(sh.rows);
-  int first = (int)blockIdx.x * a.slots;
-  auto rows_of = [&](int n) -> int { return !p.idle && n < a.n_all && n >= 0 ? a.n_heads - p.part : 0; };
-  // the token copied last: its number, where its first rows are and go
-  int i = 0;
-  const T* x_at = static_cast<const T*>(a.in[t]);
-  const O* g_at = static_cast<const O*>(a.grad[t]);
-  T* dx_at = static_cast<T*>(a.out[t]);
-  const long long x_stride = stride * a.in_token, g_stride = stride * a.out_token, dx_stride = stride * a.dx_token;
-  const bool one_batch = a.n_all == a.n_tokens;
-  auto copy = [&](int n, int set, bool again) {   // x of a row, then dy
-    const int rows = rows_of(n);
-    if (again && one_batch) {
-      i += stride;
-      x_at += x_stride;
-      g_at += g_stride;
-      dx_at += dx_stride;
-    } else if (rows > 0) {
+  const int t = p.t, group = (int)threadIdx.x / kLanes;
+  if ((int)threadIdx.x >= consumers) {
+    produce<T, O>(a, sh, kHasNorm, true);
+  } else {
+    const int stride = (int)gridDim.x * a.slots;
+    const uint32_t some = pairs_that_turn<kHalves>(a);
+      Row w[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      dw[u] = Row{{0ull, 0ull, 0ull, 0ull}, {0ull, 0ull, 0ull, 0ull}};
+      if (kHasNorm) w[u] = load_weight<kHalves>(a.weight[t], a.weight_dtype, a.weight_head ? min(p.part + u * a.parts, a.n_heads - 1) * kHeadDim : 0, p.c0, p.c1);
+    }
+    int n = (int)blockIdx.x * a.slots + p.slot, i = 0;
+    T* to = static_cast<T*>(a.out[t]);
+    auto there = [&](int u) -> bool { return !p.idle && n < a.n_all && n >= 0 && (kRows == 1 || p.part + u * a.parts < a.n_heads); };
+    if (there(0)) {
       int b;
       token_of(a, n, b, i);
-      x_at = static_cast<const T*>(a.in[t]) + (b * a.in_batch + i * a.in_token + p.part * a.in_head);
-      g_at = static_cast<const O*>(a.grad[t]) + (b * a.out_batch + i * a.out_token + p.part * a.out_head);
-      dx_at = static_cast<T*>(a.out[t]) + (b * a.dx_batch + i * a.dx_token + p.part * a.dx_head);
+      to += b * a.dx_batch + i * a.dx_token + p.part * a.dx_head;
     }
-    const T* x = x_at;
-    const O* g = g_at;
-    const uint32_t to = rows_shared + (uint32_t)(set * set_step) * 16u;
+    const int over = stride / a.n_tokens, step = stride - over * a.n_tokens;   // to the block's next tokens: batch elements, tokens
+    const long long to_step = over * a.dx_batch + step * a.dx_token;
+    const int x_bytes = kHasNorm ? kHeadDim * (int)sizeof(T) : 0, g_bytes = kHeadDim * (int)sizeof(O), token_bytes = a.n_heads * (x_bytes + g_bytes);
+    const uint8_t* rows = sh.rows + p.set * token_bytes;
+    int stage = 0;
+    for (int it = 0, first = (int)blockIdx.x * a.slots; first < a.n_all; ++it) {
+      block_barrier();
+      Row x[kRows], g[kRows];
+      float ss[kRows], hx[kRows];
+      {
+        const Turn turn = turn_of<kHalves, true>(sh.turns + ((it & 1) * a.slots + p.slot) * 3 * kPairs, some, a.first_token + i < a.n_video);
+        const uint8_t* set = rows + stage * a.slots * a.tensors * token_bytes;
 #pragma unroll
-    for (int u = 0; u < kRows; ++u, x += x_step, g += g_step) {
-      if (u * a.parts >= rows) break;
-      if constexpr (kHasNorm) copy_row(to + (uint32_t)(u * row_step) * 16u, x, p.c0, p.c1);
-      copy_row(to + (uint32_t)(u * row_step + x_words) * 16u, g, p.c0, p.c1);
-    }
-  };
-  if (per_group * a.parts != a.n_heads) clear_rows(sh.rows, a.sets * per_group * (kWords + kGradWords));
-  auto weight = [&](int u) -> Row {
-    if constexpr (!kHeadWeights) return weight_of<float, kHalves>(sh.weights, t * kHeadDim, p.c0, p.c1);
-    return load_weight<kHalves>(a.weight[t], a.weight_dtype, min(p.part + u * a.parts, a.n_heads - 1) * kHeadDim, p.c0, p.c1);
-  };
-  copy(first + p.slot, 0, false);
-  copies_end();
-  fill_constants<kHasNorm>(a, sh, t, t + 1);
-  Row dw[kSums];
-#pragma unroll
-  for (int u = 0; u < kSums; ++u) dw[u] = Row{{0ull, 0ull, 0ull, 0ull}, {0ull, 0ull, 0ull, 0ull}};
-  __syncthreads();
-  fill_turns(a, sh.angles, first, sh.turns);
-  for (int it = 0; first < a.n_all; ++it) {
-    const int next = a.n_all - first > stride ? first + stride : a.n_all, rows = rows_of(first + p.slot);
-    const int i_here = i;
-    T* to = dx_at;
-    const uint4* mine = sh.rows;
-    if (a.sets == 2) {
-      if (next < a.n_all) copy(next + p.slot, (it + 1) & 1, true);
-      copies_end();
-      copies_wait<1>();
-      mine += (it & 1) * set_step;
-    } else {
-      copies_wait<0>();
-    }
-    __syncthreads();   // these tokens' turns are there, and nobody reads those of the token before any more
-    const Turn turn = turn_of<kHalves>(a, sh.turns + ((it & 1) * a.slots + p.slot) * 2 * kPairs, a.first_token + i_here < a.n_video);
-    const bool all = __all_sync(0xffffffffu, turn.some == 255u);
-    Row w;
-    if (kHasNorm && !kHeadWeights) w = weight(0);
-    float ss = 0.f, hx = 0.f;
-    if constexpr (kNorm == PSA_NORM_TOKEN) {
-#pragma unroll 1
-      for (int u = 0; u < per_group; ++u) {
-        const Row x = row_of<T, kHalves>(read_row<T>(mine + u * row_step));
-        const Row g = rotate<true>(turn, all, row_of<O, kHalves>(read_row<O>(mine + u * row_step + x_words)));
-        if constexpr (kHeadWeights) w = weight(u);
-        ss += dot(x, x);
-        hx += dot(times(g, w), x);
-      }
-      float* sums = sh.sums + (it & 1) * 2 * groups;
-      const float s = lanes_sum2(ss, hx);
-      if ((threadIdx.x & 3) == 0) sums[((threadIdx.x >> 2) & 1) * groups + group] = s;
-      if (next < a.n_all) fill_turns(a, sh.angles, next, sh.turns + ((it + 1) & 1) * a.slots * 2 * kPairs);
-      __syncthreads();
-      ss = token_sum(a, p, sums);
-      hx = token_sum(a, p, sums + groups);
-    } else if (next < a.n_all) {
-      fill_turns(a, sh.angles, next, sh.turns + ((it + 1) & 1) * a.slots * 2 * kPairs);
-    }
-#pragma unroll
-    for (int u = 0; u < kRows; ++u, to += dx_step) {
-      if (u == per_group) break;
-      Row g = rotate<true>(turn, all, row_of<O, kHalves>(read_row<O>(mine + u * row_step + x_words)));
-      if constexpr (kHasNorm) {
-        const Row x = row_of<T, kHalves>(read_row<T>(mine + u * row_step));
-        if constexpr (kHeadWeights) w = weight(u);
-        const Row h = times(g, w);
-        if constexpr (kNorm == PSA_NORM_HEAD) {
-          ss = lanes_sum(dot(x, x));
-          hx = lanes_sum(dot(h, x));
-        }
-        const float r = rsqrtf(ss * a.inv_count + a.eps), coef = -r * r * (hx * a.inv_count);
-        const f2 rr = pack(r, r), cc = pack(coef, coef);
-        if (u * a.parts < rows) {
-          Row& d = dw[kHeadWeights ? u : 0];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            d.a[k] = fma(g.a[k], mul(x.a[k], rr), d.a[k]);
-            d.b[k] = fma(g.b[k], mul(x.b[k], rr), d.b[k]);
-            g.a[k] = mul(fma(x.a[k], cc, h.a[k]), rr);
-            g.b[k] = mul(fma(x.b[k], cc, h.b[k]), rr);
+        for (int u = 0; u < kRows; ++u) {
+          const int head = kRows == 1 ? p.part : min(p.part + u * a.parts, a.n_heads - 1);
+          Raw<O> raw_g;
+          load_row(reinterpret_cast<const O*>(set + a.n_heads * x_bytes + head * g_bytes), p.c0, p.c1, raw_g);
+          g[u] = rotate<true>(turn, row_of<O, kHalves>(raw_g));
+          if constexpr (kHasNorm) {
+            Raw<T> raw_x;
+            load_row(reinterpret_cast<const T*>(set + head * x_bytes), p.c0, p.c1, raw_x);
+            x[u] = row_of<T, kHalves>(raw_x);
+            ss[u] = dot(x[u], x[u]);
+            hx[u] = dot(times(g[u], w[u]), x[u]);
+            if constexpr (kNorm == PSA_NORM_HEAD) {
+              ss[u] = lanes_sum(ss[u]);
+              hx[u] = lanes_sum(hx[u]);
+            }
           }
         }
       }
-      if (u * a.parts < rows) store_row<T, kHalves>(to, p.c0, p.c1, g);
+      if constexpr (kNorm == PSA_NORM_TOKEN) {
+        float2* sums = sh.sums + (it & 1) * kMaxGroups;
+        const bool both = kRows > 1 && p.part + a.parts < a.n_heads;
+        const float s = lanes_sum2(both ? ss[0] + ss[kRows - 1] : ss[0], both ? hx[0] + hx[kRows - 1] : hx[0]);
+        if ((threadIdx.x & 3) == 0) reinterpret_cast<float*>(sums + group)[(threadIdx.x >> 2) & 1] = s;
+        consumer_barrier();
+        const float2 v = token_sum(sums + p.set * a.parts, a.parts);
+        ss[0] = ss[kRows - 1] = v.x;
+        hx[0] = hx[kRows - 1] = v.y;
+      }
+      if (a.stages == 1) block_barrier();
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        if (!there(u)) continue;
+        if constexpr (kHasNorm) {
+          const float r = rsqrtf(ss[u] * a.inv_count + a.eps), coef = -r * r * (hx[u] * a.inv_count);
+          const f2 rr = pack(r, r), cc = pack(coef, coef);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            dw[u].a[k] = fma(g[u].a[k], mul(x[u].a[k], rr), dw[u].a[k]);
+            dw[u].b[k] = fma(g[u].b[k], mul(x[u].b[k], rr), dw[u].b[k]);
+            g[u].a[k] = mul(fma(x[u].a[k], cc, mul(g[u].a[k], w[u].a[k])), rr);
+            g[u].b[k] = mul(fma(x[u].b[k], cc, mul(g[u].b[k], w[u].b[k])), rr);
+          }
+        }
+        store_row<T, kHalves>(to + u * a.parts * a.dx_head, p.c0, p.c1, g[u]);
+      }
+      first = a.n_all - first > stride ? first + stride : a.n_all;
+      n = first + p.slot;
+      i += step;
+      to += to_step;
+      if (i >= a.n_tokens) {
+        i -= a.n_tokens;
+        to += a.dx_batch - a.n_tokens * a.dx_token;
+      }
+      stage = stage + 1 == a.stages ? 0 : stage + 1;
     }
-    if (a.sets == 1 && next < a.n_all) {
-      copy(next + p.slot, 0, true);
-      copies_end();
-    }
-    first = next;
   }
   if (!kHasNorm || a.dw_part == nullptr) return;
   // the block's tokens, and for a shared weight its heads, in order
-  float* dw_part = reinterpret_cast<float*>(sm);   // [groups][128] of one row
-  float* to = a.dw_part + ((long long)t * gridDim.x + blockIdx.x) * a.weight_cols;
+  if (kRows > 1 && a.weight_head == 0) {
 #pragma unroll
-  for (int u = 0; u < kSums; ++u) {
-    if (u > 0 && u * a.parts >= a.n_heads) break;
-    __syncthreads();
-    store_row<float, kHalves>(dw_part + group * kHeadDim, p.c0, p.c1, dw[u]);
-    __syncthreads();
-    if (!kHeadWeights) {
-      for (int c = (int)threadIdx.x; c < kHeadDim; c += (int)blockDim.x) {
-        float s = 0.f;
-        for (int j = 0; j < groups; ++j) s += dw_part[j * kHeadDim + c];   // (idle groups left zeros)
-        to[c] = s;
-      }
-    } else {
-      for (int k = (int)threadIdx.x; k < a.parts * kHeadDim; k += (int)blockDim.x) {
-        const int head = k / kHeadDim + u * a.parts;
+    for (int k = 0; k < 4; ++k) {
+      dw[0].a[k] = fma(dw[kRows - 1].a[k], pack(1.f, 1.f), dw[0].a[k]);
+      dw[0].b[k] = fma(dw[kRows - 1].b[k], pack(1.f, 1.f), dw[0].b[k]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kRows; ++u) {
+    if (u > 0 && a.weight_head == 0) break;
+    block_barrier();
+    if ((int)threadIdx.x < consumers) store_row<float, kHalves>(dw_part + group * kHeadDim, p.c0, p.c1, dw[u]);
+    block_barrier();
+    for (int k = 0; k < a.tensors; ++k) {
+      const int tensor = a.tensors == 2 ? k : (int)blockIdx.y, per = a.tensors * a.parts * kHeadDim;   // from a token's sums to the next one's
+      float* to = a.dw_part + ((long long)tensor * gridDim.x + blockIdx.x) * a.weight_cols;
+      const float* from = dw_part + k * a.parts * kHeadDim;
+      for (int e = (int)threadIdx.x; e < (a.weight_head == 0 ? kHeadDim : a.parts * kHeadDim); e += (int)blockDim.x) {
+        const int head = e / kHeadDim + u * a.parts;
         if (head >= a.n_heads) break;
-        float s = 0.f;
-        for (int j = 0; j < a.slots; ++j) s += dw_part[j * a.parts * kHeadDim + k];
-        to[head * kHeadDim + k % kHeadDim] = s;
+        float sum = 0.f;
+        for (int j = 0; j < a.slots; ++j)
+          for (int h = 0; h < (a.weight_head == 0 ? a.parts : 1); ++h) sum += from[j * per + h * kHeadDim + e];
+        to[head * kHeadDim + e % kHeadDim] = sum;
       }
     }
   }
@@ -711,19 +717,22 @@ cudaError_t blocks_at_once(void (*kernel)(NormRopeArgs), int threads, size_t sme
   return cudaSuccess;
 }
 
-template <class T, class O, int kNorm, bool kHalves, bool kHeadWeights>
-cudaError_t launch_bwd(NormRopeArgs& a, int threads, int blocks, int n_sms, int* launched, cudaStream_t st) {
-  auto* kernel = norm_rope_bwd_kernel<T, O, kNorm, kHalves, kHeadWeights>;
-  const int words = a.rows * (int)((kNorm != PSA_NORM_NONE ? sizeof(T) : 0) + sizeof(O));
-  a.sets = sets_of(a.slots, threads, words);
-  const size_t rows = shared_bytes(a.slots, threads, words, a.sets),
-               sums = (size_t)(threads / kLanes) * kHeadDim * sizeof(float), smem = rows > sums ? rows : sums;
-  const int tensors = a.grad[1] ? 2 : 1;
+template <class T, class O, int kNorm, bool kHalves, int kRows>
+cudaError_t launch_rows(NormRopeArgs& a, bool backward, int threads, int blocks, int n_sms, int* launched, cudaStream_t st) {
+  auto* kernel = backward ? norm_rope_bwd_kernel<T, O, kNorm, kHalves, kRows> : norm_rope_kernel<T, O, kNorm, kHalves, kRows>;
+  // as many sets of rows as fit, beside as many blocks as there are registers for
+  const int bytes = a.slots * a.tensors * a.n_heads * kHeadDim * (int)(backward ? (kNorm != PSA_NORM_NONE ? sizeof(T) : 0) + sizeof(O) : sizeof(T));
+  const size_t sums = backward ? (size_t)((threads - kProducers) / kLanes) * kHeadDim * sizeof(float) : 0;
+  const size_t share = kMaxSmemBytes / (65536 / ((backward ? kBwdRegs : kRegs) * threads)) - 1024;
+  for (a.stages = kMaxStages; a.stages > 2 && shared_bytes(a.slots, bytes, a.stages) > share; --a.stages) {}
+  while (a.stages > 1 && shared_bytes(a.slots, bytes, a.stages) > kMaxSmemBytes) --a.stages;
+  const size_t rows = shared_bytes(a.slots, bytes, a.stages), smem = rows > sums ? rows : sums;
   int most;
   const cudaError_t e = blocks_at_once(kernel, threads, smem, n_sms, &most);
   if (e != cudaSuccess) return e;
-  most /= tensors;
-  if (most > kNormRopeBwdBlocks) most = kNormRopeBwdBlocks;
+  const int tensors = a.out[1] && a.tensors == 1 ? 2 : 1;   // each with blocks of its own
+  most = most > tensors ? most / tensors : 1;
+  if (backward && most > kNormRopeBwdBlocks) most = kNormRopeBwdBlocks;
   *launched = blocks < most ? blocks : most;
   kernel<<<dim3(*launched, tensors), threads, smem, st>>>(a);
   return cudaGetLastError();
@@ -731,21 +740,8 @@ cudaError_t launch_bwd(NormRopeArgs& a, int threads, int blocks, int n_sms, int*
 
 template <class T, class O, int kNorm, bool kHalves>
 cudaError_t launch_typed(NormRopeArgs& a, bool backward, int threads, int blocks, int n_sms, int* launched, cudaStream_t st) {
-  if (backward) {
-    if constexpr (kNorm != PSA_NORM_NONE) {
-      if (a.weight_head != 0) return launch_bwd<T, O, kNorm, kHalves, true>(a, threads, blocks, n_sms, launched, st);
-    }
-    return launch_bwd<T, O, kNorm, kHalves, false>(a, threads, blocks, n_sms, launched, st);
-  }
-  const int words = 2 * a.rows * (int)sizeof(T);
-  a.sets = sets_of(a.slots, threads, words);
-  const size_t smem = shared_bytes(a.slots, threads, words, a.sets);
-  int most;
-  const cudaError_t e = blocks_at_once(norm_rope_kernel<T, O, kNorm, kHalves>, threads, smem, n_sms, &most);
-  if (e != cudaSuccess) return e;
-  *launched = blocks < most ? blocks : most;
-  norm_rope_kernel<T, O, kNorm, kHalves><<<*launched, threads, smem, st>>>(a);
-  return cudaGetLastError();
+  return a.parts == a.n_heads ? launch_rows<T, O, kNorm, kHalves, 1>(a, backward, threads, blocks, n_sms, launched, st)
+                              : launch_rows<T, O, kNorm, kHalves, 2>(a, backward, threads, blocks, n_sms, launched, st);
 }
 template <class T, class O, int kNorm>
 cudaError_t launch_pairs(NormRopeArgs& a, bool halves, bool backward, int threads, int blocks, int n_sms, int* launched, cudaStream_t st) {
@@ -765,16 +761,12 @@ cudaError_t launch_norm(NormRopeArgs& a, int norm, bool halves, bool backward, i
 
 cudaError_t launch_norm_rope(NormRopeArgs& a, const psa_qk& prob, bool halves, bool backward, int n_sms, float* q_dw, float* k_dw, cudaStream_t st,
                              int* launches) {
-  // Groups a token: so many that each has at most kRows heads; one a head where there are too few tokens to fill the GPU
-  // with less.  Tokens a block: blocks of some 256 threads, whole warps.
-  const int most = (backward ? 2 : 1) * kMaxThreads / kLanes;   // groups of a block
-  const long long by_rows = (long long)a.n_all * ((a.n_heads + kRows - 1) / kRows);
-  a.parts = by_rows * kLanes < (long long)n_sms * 1024 && a.n_heads <= most ? a.n_heads : (a.n_heads + kRows - 1) / kRows;
-  if (a.parts > most) a.parts = (a.n_heads + 2 * kRows - 1) / (2 * kRows);
-  a.rows = (a.n_heads + a.parts - 1) / a.parts;
-  a.slots = 256 / (a.parts * kLanes);
+  // Groups a token: one a head, or one for two.  Tokens a block: blocks of some 256 threads, whole warps.
+  a.parts = a.n_heads <= kMaxGroups ? a.n_heads : (a.n_heads + 1) / 2;
+  a.tensors = a.out[1] && 2 * a.parts * kLanes <= kBlockThreads ? 2 : 1;
+  a.slots = kSmallThreads / (a.tensors * a.parts * kLanes);
   if (a.slots < 1) a.slots = 1;
-  const int threads = (a.slots * a.parts * kLanes + 31) & ~31, blocks = (int)(((long long)a.n_all + a.slots - 1) / a.slots);
+  const int threads = ((a.slots * a.tensors * a.parts * kLanes + 31) & ~31) + kProducers, blocks = (int)(((long long)a.n_all + a.slots - 1) / a.slots);
   int launched = 0;
   cudaError_t e;
   const int in = prob.dtype, out = prob.out_dtype;

@@ -27,7 +27,8 @@ struct NormRopeArgs {
   long long n_video;                // tokens of the sequence that are rotated: T * H * W
   long long first_token;            // of the sequence
   int n_tokens, n_all, n_heads;     // tokens of a batch element, of all of them
-  int parts, slots, rows, sets;     // groups of a token; tokens of a block; rows (heads) of a group; sets of tokens in shared memory
+  int parts, slots, stages;         // groups of a token and tensor; tokens of a block; sets of rows in shared memory
+  int tensors;                      // 2: a block takes q and k, 1: one of them
   int weight_dtype, weight_head;    // weight_head: 1 if every head has weights of its own
   int weight_cols;                  // weights
   float eps, inv_count;             // inv_count: 1 / values of a mean
@@ -39,7 +40,7 @@ struct NormRopeArgs {
   long long in_batch, in_head, in_token, out_batch, out_head, out_token, dx_batch, dx_head, dx_token;   // strides, in elements
 };
 
-// Launches the forward pass or the gradient.  The arguments have been checked; parts, slots, rows and sets are chosen here.
+// Launches the forward pass or the gradient.  The arguments have been checked; parts, slots, stages and tensors are chosen here.
 cudaError_t launch_norm_rope(NormRopeArgs& a, const psa_qk& prob, bool halves, bool backward, int n_sms, float* q_dw, float* k_dw, cudaStream_t st,
                              int* launches);
 
