@@ -125,6 +125,21 @@ struct AttnParamsCut : AttnParams {
   uint8_t order[8];
 };
 
+// Division of numbers below 2^31 by a constant d: a shift for powers of two (m == 0), else the high half of a product, shifted.
+struct Divisor {
+  uint32_t m;
+  int shift;
+};
+inline Divisor divisor_of(int d) {
+  int l = 0;
+  while ((1ll << l) < d) ++l;
+  if ((1ll << l) == d) return Divisor{0u, l};
+  return Divisor{(uint32_t)((1ull << (31 + l)) / (unsigned)d + 1), l - 1};   // n < 2^31: exact, as m d - 2^(31 + l) <= d <= 2^l
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ int divide(int n, const Divisor& d) { return d.m == 0u ? n >> d.shift : (int)(__umulhi((uint32_t)n, d.m) >> d.shift); }
+#endif
+
 // Blocks that psa_select_blocks keeps for each query block of a head, and the head's first entry of col_idx.
 struct SelectHeads {
   int keep[kMaxHeads], base[kMaxHeads];

@@ -258,9 +258,6 @@ __device__ __forceinline__ Place place_of(const NormRopeArgs& a) {
   return p;
 }
 
-// n / d for n below 2^31 (NormRopeArgs::Divisor).
-__device__ __forceinline__ int divide(int n, const Divisor& d) { return d.m == 0u ? n >> d.shift : (int)(__umulhi((uint32_t)n, d.m) >> d.shift); }
-
 // Token n of all batch elements: batch element and token within it.
 __device__ __forceinline__ void token_of(const NormRopeArgs& a, int n, int& b, int& i) {
   b = a.n_all == a.n_tokens ? 0 : divide(n, a.by_tokens);

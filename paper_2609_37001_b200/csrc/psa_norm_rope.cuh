@@ -6,18 +6,6 @@ namespace psa {
 
 constexpr int kNormRopeBwdBlocks = 444;   // most blocks a tensor in a gradient launch, each with a partial sum per weight
 
-// Division of numbers below 2^31 by a constant d: a shift for powers of two (m == 0), else the high half of a product, shifted.
-struct Divisor {
-  uint32_t m;
-  int shift;
-};
-inline Divisor divisor_of(int d) {
-  int l = 0;
-  while ((1ll << l) < d) ++l;
-  if ((1ll << l) == d) return Divisor{0u, l};
-  return Divisor{(uint32_t)((1ull << (31 + l)) / (unsigned)d + 1), l - 1};   // n < 2^31: exact, as m d - 2^(31 + l) <= d <= 2^l
-}
-
 struct NormRopeArgs {
   double turns[64];                 // quarter turns per unit of position of every pair, axis after axis
   Divisor by_tokens, by_w, by_h;

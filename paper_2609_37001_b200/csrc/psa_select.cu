@@ -6,8 +6,8 @@
 // order some 1 in 10^4 rows of a 315-block head otherwise).  Equal scores (exactly, whatever the blocks: the sums are the same
 // operations) go to the lowest block.
 //
-// Two kernels: pooling is bound by reading q and k once; scores and choice together keep a tile of rows of scores in shared memory,
-// so that the heads * NB^2 scores of 8 bytes never reach HBM.
+// Two kernels: pooling is bound by reading q and k once; scores and choice together keep the scores of eight rows in shared memory, so
+// that the heads * NB^2 scores of 8 bytes never reach HBM.
 #include <cuda_bf16.h>
 
 #include "psa_common.cuh"
@@ -17,7 +17,8 @@ namespace psa {
 namespace {
 
 constexpr int kPoolThreads = 256, kPoolRows = kPoolThreads / 16;   // 16 lanes a token, 8 channels each
-constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
+constexpr int kPoolAhead = 4;                                      // pairs of tokens that a thread has on their way
+constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32, kSelectRows = 8;
 constexpr int kSumPitch = kHeadDim + 2;   // doubles a row of Q in shared memory
 
 struct BlockOrigin {
@@ -31,37 +32,100 @@ __device__ __forceinline__ BlockOrigin block_origin(const Geom& g, int b) {
   return o;
 }
 
-// Sums over the tokens of one block of one head of q (z = 0) or k (z = 1).
+// Sums over the tokens of one block of one head of q (z = 0) or k (z = 1).  Bound by HBM (q and k once), if the conversions to 64
+// bits allow: at 16 a clock and SM they alone took 1.4 times as long.  So of the two values in a 32-bit word only the lower one is
+// converted.  The bits of the upper one are moved three places down, under the sign: read as the upper half of a double that is the value
+// times 2^-896, exactly (subnormals, too), which the sum is multiplied back by.  Infinities and NaN would become numbers; a
+// thread that saw an exponent of 255 adds its values up again by conversion.
+__device__ __forceinline__ double upper_scaled(uint32_t v) { return __hiloint2double(((int)v >> 3) & 0x8fffe000, 0); }
+__device__ __forceinline__ double lower(uint32_t v) { return (double)__uint_as_float(v << 16); }
+__device__ __forceinline__ double upper(uint32_t v) { return (double)__uint_as_float(v & 0xffff0000u); }
 __global__ void __launch_bounds__(kPoolThreads)
 pool_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ k, const Geom g, long long stride_head, long long stride_token,
             double* __restrict__ sums) {
-  __shared__ double part[kPoolRows][kHeadDim];
+  __shared__ __align__(16) union {
+    uint4 copied[2 * kPoolAhead][kPoolThreads];
+    double part[kPoolRows][kHeadDim];
+  } sm;
   const int b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 15, row = threadIdx.x >> 4;
   const BlockOrigin o = block_origin(g, b);
-  const __nv_bfloat16* from = (blockIdx.z ? k : q) + head * stride_head + 8 * lane;
-  const int frame = o.nh * o.nw, n = o.nt * frame;
+  const __nv_bfloat16* from = (blockIdx.z ? k : q) + head * stride_head + (((long long)o.t0 * g.H + o.h0) * g.W + o.w0) * stride_token + 8 * lane;
+  // 16 lanes take a line of the block's tokens, or (fewer than 16 lines) a part of one, then the 16th behind it: addresses go up by one
+  // token, and only a new line is looked for
+  const int lines = o.nt * o.nh, log_parts = lines >= 16 ? 0 : (lines >= 8 ? 1 : (lines >= 4 ? 2 : (lines >= 2 ? 3 : 4)));
+  const int part_len = (o.nw + (1 << log_parts) - 1) >> log_parts, units = lines << log_parts;
+  auto len_of = [&](int u) -> int { return max(0, min(part_len, o.nw - (u & ((1 << log_parts) - 1)) * part_len)); };
+  auto start_of = [&](int u) -> const __nv_bfloat16* {
+    const int line = u >> log_parts, t = line / o.nh, h = line - t * o.nh;
+    return from + ((long long)(t * g.H + h) * g.W + (u & ((1 << log_parts) - 1)) * part_len) * stride_token;
+  };
+  int total = 0;   // tokens of these lanes
+  for (int u = row; u < units; u += kPoolRows) total += len_of(u);
+  // two tokens at a time, kPoolAhead pairs on their way to shared memory, where each thread reads what it copied; zeros behind the last
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&sm.copied[0][threadIdx.x]);
+  int unit = row, left = 0, fetched = 0;
+  const __nv_bfloat16* at = from;
+  auto fetch = [&](int pair) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool there = fetched < total;
+      if (there && left == 0) {
+        do { left = len_of(unit); unit += kPoolRows; } while (left == 0);   // (there is another token)
+        at = start_of(unit - kPoolRows);
+      }
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                   ::"r"(mine + (uint32_t)((2 * pair + i) * kPoolThreads) * 16u), "l"(at), "r"(there ? 16 : 0) : "memory");
+      if (there) {
+        ++fetched;
+        if (--left > 0) at += stride_token;
+      }
+    }
+  };
   double acc[8];
+  float most[4] = {0.f, 0.f, 0.f, 0.f};   // largest magnitude among the upper values (and what lies below them in the word), or NaN
 #pragma unroll
   for (int c = 0; c < 8; ++c) acc[c] = 0.0;
-#pragma unroll 4
-  for (int r = row; r < n; r += kPoolRows) {
-    const int t = r / frame, y = r - t * frame, h = y / o.nw, w = y - h * o.nw;
-    const long long token = ((long long)(o.t0 + t) * g.H + o.h0 + h) * g.W + o.w0 + w;
-    const uint4 x = *reinterpret_cast<const uint4*>(from + token * stride_token);
-    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+  auto add = [&](const uint4& x, const uint4& y) {
+    const uint32_t v[4] = {x.x, x.y, x.z, x.w}, u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      acc[2 * c] += (double)__uint_as_float(v[c] << 16);
-      acc[2 * c + 1] += (double)__uint_as_float(v[c] & 0xffff0000u);
+      acc[2 * c] += lower(v[c]);
+      acc[2 * c + 1] += upper_scaled(v[c]);
+      acc[2 * c] += lower(u[c]);
+      acc[2 * c + 1] += upper_scaled(u[c]);
+      asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(most[c]) : "f"(fabsf(__uint_as_float(v[c]))), "f"(fabsf(__uint_as_float(u[c]))));
     }
+  };
+#pragma unroll
+  for (int i = 0; i < kPoolAhead; ++i) {
+    if (fetched < total) fetch(i);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  for (int n = 0, pair = 0; n < total; n += 2, pair = pair + 1 == kPoolAhead ? 0 : pair + 1) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kPoolAhead - 1) : "memory");
+    add(sm.copied[2 * pair][threadIdx.x], sm.copied[2 * pair + 1][threadIdx.x]);
+    if (fetched < total) fetch(pair);
+    asm volatile("cp.async.commit_group;" ::: "memory");
   }
 #pragma unroll
-  for (int c = 0; c < 8; ++c) part[row][8 * lane + c] = acc[c];
+  for (int c = 0; c < 4; ++c) {
+    acc[2 * c + 1] *= 0x1p896;
+    if (!(most[c] < __uint_as_float(0x7f800000u))) {
+      acc[2 * c + 1] = 0.0;
+      for (int u = row; u < units; u += kPoolRows) {
+        const __nv_bfloat16* x = start_of(u);
+        for (int n = len_of(u); n > 0; --n, x += stride_token) acc[2 * c + 1] += upper(reinterpret_cast<const uint32_t*>(x)[c]);
+      }
+    }
+  }
+  __syncthreads();   // (nobody reads copies any more)
+#pragma unroll
+  for (int c = 0; c < 8; ++c) sm.part[row][8 * lane + c] = acc[c];
   __syncthreads();
   if (threadIdx.x < kHeadDim) {
     double s = 0.0;
 #pragma unroll
-    for (int r = 0; r < kPoolRows; ++r) s += part[r][threadIdx.x];
+    for (int r = 0; r < kPoolRows; ++r) s += sm.part[r][threadIdx.x];
     sums[(((long long)blockIdx.z * gridDim.y + head) * g.NB + b) * kHeadDim + threadIdx.x] = s;
   }
 }
@@ -77,20 +141,72 @@ __device__ __forceinline__ unsigned long long order_key(double s) {
   return (unsigned long long)b ^ (b < 0 ? ~0ull : 1ull << 63);
 }
 
-// kTiles * 8 query blocks of one head: their scores against every key block, then one warp a row chooses.
-template <int kTiles>
+// The list of one row by one warp: `n` of its keys (in shared memory) to `to`.  kHeld: 32-key pieces that a lane keeps in registers
+// during the search, 0: none, it reads them every time.
+template <int kHeld>
+__device__ __forceinline__ void choose(const unsigned long long* row, int nb, int n, int lane, int* to) {
+  unsigned long long held[kHeld ? kHeld : 1];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = lane + 32 * i < nb ? row[lane + 32 * i] : 0ull;
+  // keys that f holds for, of all lanes (not for 0, which stands behind the last key)
+  auto count = [&](auto f) -> int {
+    int c = 0;
+    if constexpr (kHeld > 0) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) c += f(held[i]);
+    } else {
+      for (int j = lane; j < nb; j += 32) c += f(row[j]);
+    }
+    return __reduce_add_sync(0xffffffffu, c);
+  };
+  // the n-th largest key lies in [lo, hi]: at least n keys are >= lo, fewer are > hi.  Halved until exactly n keys are >= lo, or
+  // nothing is left between.
+  unsigned long long lo = ~0ull, hi = 0;
+  for (int j = lane; j < nb; j += 32) {
+    lo = min(lo, row[j]);
+    hi = max(hi, row[j]);
+  }
+#pragma unroll
+  for (int m = 16; m > 0; m >>= 1) {
+    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, m));
+    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, m));
+  }
+  int at_least = nb;   // keys >= lo
+  while (at_least != n && lo < hi) {
+    const unsigned long long mid = lo + (hi - lo) / 2 + 1;   // above lo, at most hi
+    const int c = count([&](unsigned long long key) { return key >= mid; });
+    if (c >= n) { lo = mid; at_least = c; }
+    else hi = mid - 1;
+  }
+  // all keys above lo, and the first ones equal to it as far as there is room (no key is 0)
+  int room = at_least == n ? nb : n - count([&](unsigned long long key) { return key > lo; });
+  for (int j0 = 0; j0 < nb; j0 += 32) {
+    const int j = j0 + lane;
+    const unsigned long long key = j < nb ? row[j] : 0ull;
+    const unsigned equal = __ballot_sync(0xffffffffu, key == lo), more = __ballot_sync(0xffffffffu, key > lo);
+    const unsigned below = (1u << lane) - 1u;
+    const bool take = (more >> lane & 1u) || ((equal >> lane & 1u) && __popc(equal & below) < room);
+    const unsigned taken = __ballot_sync(0xffffffffu, take);
+    room -= min(room, __popc(equal));
+    if (take) to[__popc(taken & below)] = j;
+    to += __popc(taken);
+  }
+}
+
+// Eight query blocks of one head: their scores against every key block, then one warp a row chooses.  Bound by the waits in both
+// parts; several blocks an SM overlap them.  (16 query blocks read the key sums half as often, but only two blocks fit an SM then: 24
+// heads of 450 blocks 378 instead of 371 us for the whole call; two rows a warp in turn: 395.)
 __global__ void __launch_bounds__(kSelectThreads)
 select_kernel(const double* __restrict__ sums, const Geom g, const __grid_constant__ SelectHeads heads, int keep_self, int* __restrict__ row_ptr,
               int* __restrict__ col_idx) {
-  constexpr int kRows = 8 * kTiles;
   extern __shared__ __align__(16) double sm[];
-  double* qs = sm;                                                            // [kRows][kSumPitch]
-  unsigned long long* keys = reinterpret_cast<unsigned long long*>(sm + kRows * kSumPitch);   // [kRows][NB]
-  const int head = blockIdx.y, i0 = blockIdx.x * kRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows = min(kRows, g.NB - i0);
+  double* qs = sm;                                                                                   // [kSelectRows][kSumPitch]
+  unsigned long long* keys = reinterpret_cast<unsigned long long*>(sm + kSelectRows * kSumPitch);   // [kSelectRows][NB]
+  const int head = blockIdx.y, i0 = blockIdx.x * kSelectRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rows = min(kSelectRows, g.NB - i0);
   const double* q_sums = sums + ((long long)head * g.NB + i0) * kHeadDim;
   const double* k_sums = sums + ((long long)(gridDim.y + head) * g.NB) * kHeadDim;
-  for (int i = threadIdx.x; i < kRows * kHeadDim; i += kSelectThreads) {
+  for (int i = threadIdx.x; i < kSelectRows * kHeadDim; i += kSelectThreads) {
     const int r = i / kHeadDim, c = i % kHeadDim;
     qs[r * kSumPitch + c] = r < rows ? q_sums[i] : 0.0;
   }
@@ -100,30 +216,19 @@ select_kernel(const double* __restrict__ sums, const Geom g, const __grid_consta
   const int x = lane & 3, y = lane >> 2;
   for (int j0 = 8 * warp; j0 < g.NB; j0 += 8 * kSelectWarps) {
     const double2* kp = reinterpret_cast<const double2*>(k_sums + (long long)min(j0 + y, g.NB - 1) * kHeadDim + 2 * x);
-    double d[kTiles][2];
-#pragma unroll
-    for (int m = 0; m < kTiles; ++m) d[m][0] = d[m][1] = 0.0;
+    double d[2] = {0.0, 0.0};
 #pragma unroll 8
     for (int p = 0; p < kHeadDim / 8; ++p) {
-      const double2 b = kp[4 * p];
-#pragma unroll
-      for (int m = 0; m < kTiles; ++m) {
-        const double2 a = *reinterpret_cast<const double2*>(qs + (8 * m + y) * kSumPitch + 8 * p + 2 * x);
-        mma_f64(d[m], a.x, b.x);
-        mma_f64(d[m], a.y, b.y);
-      }
+      const double2 b = kp[4 * p], a = *reinterpret_cast<const double2*>(qs + y * kSumPitch + 8 * p + 2 * x);
+      mma_f64(d, a.x, b.x);
+      mma_f64(d, a.y, b.y);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int j = j0 + 2 * x + e;
       if (j >= g.NB) continue;
       const BlockOrigin o = block_origin(g, j);
-      const double n = (double)(o.nt * o.nh * o.nw);
-#pragma unroll
-      for (int m = 0; m < kTiles; ++m) {
-        const int r = 8 * m + y;
-        keys[r * g.NB + j] = keep_self && j == i0 + r ? ~0ull : order_key(d[m][e] / n);
-      }
+      keys[y * g.NB + j] = keep_self && j == i0 + y ? ~0ull : order_key(d[e] / (double)(o.nt * o.nh * o.nw));
     }
   }
   __syncthreads();
@@ -131,67 +236,21 @@ select_kernel(const double* __restrict__ sums, const Geom g, const __grid_consta
   for (int r = warp; r < rows; r += kSelectWarps) {
     const unsigned long long* mine = keys + r * g.NB;
     const int row = head * g.NB + i0 + r, base = heads.base[head] + (i0 + r) * keep;
-    // the keep-th largest key lies in [lo, hi]: at least `keep` keys are >= lo, fewer are > hi.  Halved until exactly `keep` keys
-    // are >= lo, or nothing is left between.
-    unsigned long long lo = ~0ull, hi = 0;
-    for (int j = lane; j < g.NB; j += 32) {
-      lo = min(lo, mine[j]);
-      hi = max(hi, mine[j]);
-    }
-#pragma unroll
-    for (int m = 16; m > 0; m >>= 1) {
-      lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, m));
-      hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, m));
-    }
-    int at_least = g.NB;   // keys >= lo
-    while (at_least != keep && lo < hi) {
-      const unsigned long long mid = lo + (hi - lo) / 2 + 1;   // above lo, at most hi
-      int n = 0;
-      for (int j = lane; j < g.NB; j += 32) n += mine[j] >= mid;
-      n = __reduce_add_sync(0xffffffffu, n);
-      if (n >= keep) { lo = mid; at_least = n; }
-      else hi = mid - 1;
-    }
-    // all keys above lo, and the first ones equal to it as far as there is room
-    int above = 0;
-    if (at_least != keep) {
-      for (int j = lane; j < g.NB; j += 32) above += mine[j] > lo;
-      above = __reduce_add_sync(0xffffffffu, above);
-    }
-    int room = at_least == keep ? g.NB : keep - above, at = base;
-    for (int j0 = 0; j0 < g.NB; j0 += 32) {
-      const int j = j0 + lane;
-      const unsigned long long key = j < g.NB ? mine[j] : 0ull;
-      const unsigned equal = __ballot_sync(0xffffffffu, j < g.NB && key == lo), more = __ballot_sync(0xffffffffu, j < g.NB && key > lo);
-      const unsigned below = (1u << lane) - 1u;
-      const bool take = (more >> lane & 1u) || ((equal >> lane & 1u) && __popc(equal & below) < room);
-      const unsigned taken = __ballot_sync(0xffffffffu, take);
-      room -= min(room, __popc(equal));
-      if (take) col_idx[at + __popc(taken & below)] = j;
-      at += __popc(taken);
-    }
     if (lane == 0) {
       row_ptr[row] = base;
       if (i0 + r + 1 == g.NB) row_ptr[row + 1] = base + keep;   // (the next head writes the same there)
     }
+    if (g.NB <= 256) choose<8>(mine, g.NB, keep, lane, col_idx + base);
+    else if (g.NB <= 512) choose<16>(mine, g.NB, keep, lane, col_idx + base);
+    else choose<0>(mine, g.NB, keep, lane, col_idx + base);
   }
 }
 
-size_t select_smem(int rows, int nb) { return ((size_t)rows * kSumPitch + (size_t)rows * nb) * sizeof(double); }
-
-template <int kTiles>
-cudaError_t launch_select_tiles(const double* sums, const Geom& g, const SelectHeads& heads, int n_heads, bool keep_self, int* row_ptr, int* col_idx,
-                                cudaStream_t st) {
-  const size_t smem = select_smem(8 * kTiles, g.NB);
-  const cudaError_t e = cudaFuncSetAttribute(select_kernel<kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
-  select_kernel<kTiles><<<dim3((g.NB + 8 * kTiles - 1) / (8 * kTiles), n_heads), kSelectThreads, smem, st>>>(sums, g, heads, keep_self ? 1 : 0, row_ptr, col_idx);
-  return cudaGetLastError();
-}
+size_t select_smem(int nb) { return (size_t)kSelectRows * (kSumPitch + nb) * sizeof(double); }
 
 }  // namespace
 
-bool select_fits(int nb) { return select_smem(8, nb) <= kMaxSmemBytes; }
+bool select_fits(int nb) { return select_smem(nb) <= kMaxSmemBytes; }
 
 cudaError_t launch_select(const void* q, const void* k, const Geom& g, long long stride_head, long long stride_token, const SelectHeads& heads, int n_heads,
                           bool keep_self, double* sums, int* row_ptr, int* col_idx, cudaStream_t st, int* launches) {
@@ -200,9 +259,10 @@ cudaError_t launch_select(const void* q, const void* k, const Geom& g, long long
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   ++*launches;
-  // 16 rows a block read the key sums half as often as 8
-  e = select_smem(16, g.NB) <= kMaxSmemBytes ? launch_select_tiles<2>(sums, g, heads, n_heads, keep_self, row_ptr, col_idx, st)
-                                             : launch_select_tiles<1>(sums, g, heads, n_heads, keep_self, row_ptr, col_idx, st);
+  const size_t smem = select_smem(g.NB);
+  if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+  select_kernel<<<dim3((g.NB + kSelectRows - 1) / kSelectRows, n_heads), kSelectThreads, smem, st>>>(sums, g, heads, keep_self ? 1 : 0, row_ptr, col_idx);
+  e = cudaGetLastError();
   if (e == cudaSuccess) ++*launches;
   return e;
 }
