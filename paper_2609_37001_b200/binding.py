@@ -412,16 +412,17 @@ def psa_search_select_at_sparsity(losses: Sequence[float], sparsity: Sequence[fl
 
 def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
     """Device tensors of the current device (kernels are launched there)."""
-    here = None
+    here = -2
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("device tensors required")
-        if here is None:
-            here = torch._C._cuda_getDevice()
-        if t.device.index != here:
-            raise ValueError("tensors must be on the current device")
+        if t is not None:
+            index = t.get_device()   # (-1: host memory)
+            if index != here:
+                if index < 0:
+                    raise ValueError("device tensors required")
+                if here < 0:
+                    here = torch._C._cuda_getDevice()
+                if index != here:
+                    raise ValueError("tensors must be on the current device")
 
 
 def _used_on(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> None:
@@ -479,6 +480,21 @@ def _norm_rope_call(first: torch.Tensor, out: torch.Tensor, grad: Optional[torch
     dt, dh, dw = dims
     rope = _pack_rope(int(dt), int(dh), int(dw), _PAIRS[pairs], theta, *origin, *step)
     return prob, rope, weight_heads
+
+
+_SIZES: dict = {}
+
+
+def _scratch_bytes(what: str, n_heads: int, grid, tile, n_text: int = 0) -> int:
+    """Scratch of psa_select_blocks or psa_attn_fwd_lists, remembered by the call's sizes (asking takes 2 us)."""
+    key = (what, n_heads, tuple(grid), tuple(tile), n_text)
+    need = _SIZES.get(key)
+    if need is None:
+        need = psa_select_scratch_bytes(n_heads, grid, tile) if what == "select" else psa_attn_fwd_lists_scratch_bytes(n_heads, grid, tile, n_text)
+        if len(_SIZES) >= 256:
+            _SIZES.clear()
+        _SIZES[key] = need
+    return need
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -586,20 +602,18 @@ def psa_select_blocks(q: torch.Tensor, k: torch.Tensor, grid: Sequence[int], til
     if bt < 1 or bh < 1 or bw < 1:
         raise ValueError("tile extents must be positive")
     nb = -(-T // bt) * -(-H // bh) * -(-W // bw)
-    each = [int(keep)] * nh if not hasattr(keep, "__len__") else [int(x) for x in keep]
-    if len(each) != nh or min(each) < 1 or max(each) > nb:
+    each = [keep] * nh if type(keep) is int else [int(x) for x in (keep if hasattr(keep, "__len__") else [keep] * nh)]
+    if len(each) != nh or min(each, default=1) < 1 or max(each, default=1) > nb:
         raise ValueError("keep: between 1 and the number of blocks, one for all heads or one each")
     prob = _problem(nh, tile, 1.0, st[0], st[1], d)
-    need = int(lib().psa_select_scratch_bytes(prob, T, H, W))
-    if need < 0:
-        _check(need, "psa_select_blocks")
+    need = _scratch_bytes("select", nh, grid, tile)
     new = []
     if out is None:
         out = (torch.empty(nh * nb + 1, dtype=torch.int32, device=q.device), torch.empty(sum(each) * nb, dtype=torch.int32, device=q.device))
         new.extend(out)
-    row_ptr, col_idx = out
-    if any(x.dtype != torch.int32 or not x.is_contiguous() for x in out) or row_ptr.numel() != nh * nb + 1 or col_idx.numel() < sum(each) * nb:
+    elif any(x.dtype != torch.int32 or not x.is_contiguous() for x in out) or out[0].numel() != nh * nb + 1 or out[1].numel() < sum(each) * nb:
         raise ValueError("row_ptr (heads * blocks + 1 entries) and col_idx must be contiguous int32 tensors")
+    row_ptr, col_idx = out
     if scratch is None:
         scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
         new.append(scratch)
@@ -645,9 +659,7 @@ def psa_attn_fwd_lists(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_pt
         raise ValueError("out must be like q, lse fp32 [heads, tokens]")
     out, lse, st = _device_call(q, k, v, out, lse, (nh, Lt))
     prob = _problem(nh, tile, scale, st[0], st[1], d)
-    need = int(lib().psa_attn_fwd_lists_scratch_bytes(prob, n_text, T, H, W))
-    if need < 0:
-        _check(need, "psa_attn_fwd_lists")
+    need = _scratch_bytes("lists", nh, grid, tile, n_text)
     given = scratch
     if scratch is None:
         scratch = torch.empty(need, dtype=torch.uint8, device=q.device)

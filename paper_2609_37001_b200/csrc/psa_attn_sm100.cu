@@ -2101,7 +2101,7 @@ cudaError_t attn_init(int clusters[3]) {
   const void* kernels[] = {PSA_ALL_GRIDS(kTicket), PSA_ALL_GRIDS(kDirect), PSA_ALL_GRIDS(kShared), PSA_ALL_GRIDS(kSharedDirect),
                            (const void*)attn_fwd_kernel<kTicketShort, kWhole>, (const void*)attn_fwd_kernel<kTicketShort, kPadded>,
 #define PSA_LIST_GRIDS(mode) (const void*)attn_fwd_kernel<mode, kWhole, true>, (const void*)attn_fwd_kernel<mode, kPadded, true>
-                           PSA_LIST_GRIDS(kTicket), PSA_LIST_GRIDS(kDirect), PSA_LIST_GRIDS(kSharedDirect)};
+                           PSA_LIST_GRIDS(kTicket), PSA_LIST_GRIDS(kTicketShort), PSA_LIST_GRIDS(kDirect), PSA_LIST_GRIDS(kSharedDirect)};
 #undef PSA_LIST_GRIDS
 #undef PSA_ALL_GRIDS
   cudaError_t e = cudaSuccess;
@@ -2152,15 +2152,16 @@ cudaError_t launch_plan_lists(const Geom& g, const KeyLists& lists, int n_heads_
   }
   return cudaLaunchKernelEx(&lc.cfg, plan_lists_kernel, g, lists, counter, ws_header, call_id, items);
 }
-cudaError_t launch_attn_lists(const TensorMaps& tm, const AttnParamsLists& prm, int n_sms, int cluster, Grid grid, bool direct, cudaStream_t stream,
-                              Mode* mode) {
+cudaError_t launch_attn_lists(const TensorMaps& tm, const AttnParamsLists& prm, int n_sms, int cluster, Grid grid, bool direct, bool short_items,
+                              cudaStream_t stream, Mode* mode) {
   const int ctas = cluster > 1 || direct ? prm.n_items * cluster : (prm.n_items < n_sms ? prm.n_items : n_sms);
   LaunchConfig lc(ctas, kThreads, kSmemAlloc, stream, cluster);
-  *mode = cluster > 1 ? kSharedDirect : (direct ? kDirect : kTicket);
+  *mode = cluster > 1 ? kSharedDirect : (direct ? kDirect : (short_items ? kTicketShort : kTicket));
   const NoHeads none;
   auto launch = [&](auto* whole, auto* padded) { return cudaLaunchKernelEx(&lc.cfg, grid == kWhole ? whole : padded, tm, none, prm); };
   if (*mode == kSharedDirect) return launch(attn_fwd_kernel<kSharedDirect, kWhole, true>, attn_fwd_kernel<kSharedDirect, kPadded, true>);
   if (*mode == kDirect) return launch(attn_fwd_kernel<kDirect, kWhole, true>, attn_fwd_kernel<kDirect, kPadded, true>);
+  if (*mode == kTicketShort) return launch(attn_fwd_kernel<kTicketShort, kWhole, true>, attn_fwd_kernel<kTicketShort, kPadded, true>);
   return launch(attn_fwd_kernel<kTicket, kWhole, true>, attn_fwd_kernel<kTicket, kPadded, true>);
 }
 

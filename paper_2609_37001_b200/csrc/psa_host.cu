@@ -26,8 +26,8 @@ cudaError_t launch_attn(const TensorMapsCut& tm, const HeadParamsArray& heads, c
                         Grid grid, bool direct, bool short_items, bool empty_slabs, cudaStream_t stream, Mode* mode);
 cudaError_t launch_plan_lists(const Geom& g, const KeyLists& lists, int n_heads_here, int* counter, int* ws_header, int call_id, WorkItem* items,
                               cudaStream_t stream);
-cudaError_t launch_attn_lists(const TensorMaps& tm, const AttnParamsLists& prm, int n_sms, int cluster, Grid grid, bool direct, cudaStream_t stream,
-                              Mode* mode);
+cudaError_t launch_attn_lists(const TensorMaps& tm, const AttnParamsLists& prm, int n_sms, int cluster, Grid grid, bool direct, bool short_items,
+                              cudaStream_t stream, Mode* mode);
 bool select_fits(int nb);
 cudaError_t launch_select(const void* q, const void* k, const Geom& g, long long stride_head, long long stride_token, const SelectHeads& heads, int n_heads,
                           bool keep_self, double* sums, int* row_ptr, int* col_idx, cudaStream_t st, int* launches);
@@ -765,14 +765,15 @@ cudaError_t launch_call(const TensorMapsCut& tm, const AttnParams& prm, const Ho
 }
 
 // Planning (unless the launch is direct) and attention over lists.
-cudaError_t launch_lists(const TensorMaps& tm, const AttnParamsLists& prm, const HostGeom& hg, const Workspace& ws, int cluster, bool direct, cudaStream_t st) {
+cudaError_t launch_lists(const TensorMaps& tm, const AttnParamsLists& prm, const HostGeom& hg, const long long* weights, const Workspace& ws, int cluster,
+                         bool direct, cudaStream_t st) {
   if (!direct) {
     const cudaError_t e = launch_plan_lists(prm.g, prm.lists, prm.g.n_heads, prm.counter, prm.ws_header, prm.call_id, const_cast<WorkItem*>(prm.items), st);
     if (e != cudaSuccess) return e;
     ++g_launches;
   }
   if (g_ev_start && g_ev_stop) cudaEventRecord(g_ev_start, st);
-  const cudaError_t e = launch_attn_lists(tm, prm, ws.n_sms, cluster, hg.grid, direct, st, &g_last_attn.mode);
+  const cudaError_t e = launch_attn_lists(tm, prm, ws.n_sms, cluster, hg.grid, direct, short_items(hg, weights, prm.g.n_heads), st, &g_last_attn.mode);
   if (e != cudaSuccess) return e;
   ++g_launches;
   record_launch(hg, prm.n_items, cluster, true);
@@ -1147,7 +1148,7 @@ int psa_attn_fwd_lists(const void* q, const void* k, const void* v, void* out, f
     prm.counter = static_cast<int*>(scratch);
     // items shared by CTAs are taken in order, whatever their number
     const bool direct = cluster > 1 || runs_at_once(*ws, prm.n_items, cluster);
-    if (launch_lists(tm, prm, g, *ws, cluster, direct, st) != cudaSuccess) return PSA_ERR_CUDA;
+    if (launch_lists(tm, prm, g, weights.data(), *ws, cluster, direct, st) != cudaSuccess) return PSA_ERR_CUDA;
   }
   return PSA_OK;
 }
@@ -1498,7 +1499,10 @@ static int norm_rope_args(const psa_qk* prob, const psa_rope* rope, int T, int H
     if (!std::isfinite(rope->origin[x]) || !std::isfinite(rope->step[x]) || !(last * fastest < 281474976710656.0)) return PSA_ERR_INVALID_ARG;
     a->origin[x] = rope->origin[x];
     a->step[x] = rope->step[x];
-    for (int j = 0; j < dims[x] / 2; ++j) a->turns[p++] = std::pow(rope->theta, -2.0 * j / dims[x]) / 1.570796326794896619231;
+    // (every eighth by the power function, which takes 30 ns, the others from the one before: off by 8 roundings of 64 bits at most)
+    const double ratio = dims[x] ? std::pow(rope->theta, -2.0 / dims[x]) : 1.0;
+    for (int j = 0; j < dims[x] / 2; ++j, ++p)
+      a->turns[p] = j % 8 == 0 ? std::pow(rope->theta, -2.0 * j / dims[x]) / 1.570796326794896619231 : a->turns[p - 1] * ratio;
     a->pairs[x] = p;
   }
   a->H = H;

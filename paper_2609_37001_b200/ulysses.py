@@ -63,16 +63,22 @@ def local_heads(n_heads: int, group=None) -> Tuple[int, int]:
 
 def psa_attn_fwd_ulysses(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head_params: Sequence[Sequence[int]],
                          grid: Sequence[int], tile: Sequence[int], scale: float, group=None,
-                         attn_fn: Optional[Callable] = None):
+                         attn_fn: Optional[Callable] = None, norm_rope: Optional[dict] = None,
+                         norm_rope_fn: Optional[Callable] = None):
     """Stripe attention on sequence-sharded inputs.  q, k, v: [heads, L/P, 128] (this rank's token
     chunk of every head); ``head_params`` lists the masks of ALL heads.  Returns (out [heads, L/P, 128],
     lse [heads, L/P]) in the same sequence-sharded layout.
 
-    ``attn_fn(q, k, v, params, grid, tile, scale) -> (out, lse)`` defaults to ``binding.psa_attn_fwd``;
-    the CPU tests pass their own."""
-    if attn_fn is None:
+    ``norm_rope``: options of ``binding.psa_qk_norm_rope`` (dims, norm, weights of all heads, ...).  With it q and k
+    are normed and rotated here first, where a rank still holds all heads of its tokens, which a mean over all
+    heads needs; the options do not name the tokens, which are this rank's.
+
+    ``attn_fn(q, k, v, params, grid, tile, scale) -> (out, lse)`` defaults to ``binding.psa_attn_fwd``,
+    ``norm_rope_fn`` to ``binding.psa_qk_norm_rope``; the CPU tests pass their own."""
+    if attn_fn is None or (norm_rope is not None and norm_rope_fn is None):
         from . import binding
-        attn_fn = binding.psa_attn_fwd
+        attn_fn = attn_fn or binding.psa_attn_fwd
+        norm_rope_fn = norm_rope_fn or binding.psa_qk_norm_rope
     nh = q.shape[0]
     if len(head_params) != nh:
         raise ValueError("one parameter set per head")
@@ -80,6 +86,11 @@ def psa_attn_fwd_ulysses(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head
     T, H, W = (int(x) for x in grid)
     if q.shape[1] * P != T * H * W:
         raise ValueError("local token count times group size must equal T*H*W")
+    if norm_rope is not None:
+        if "first_token" in norm_rope or "out" in norm_rope or norm_rope.get("n_text", 0):
+            raise ValueError("norm_rope: this rank's video tokens, into new tensors")
+        rank = dist.get_rank(group) if P > 1 else 0
+        q, k = norm_rope_fn(q, k, grid, first_token=rank * q.shape[1], **norm_rope)
     qh, kh, vh = (seq_to_head_shards(t, group) for t in (q, k, v))
     lo, hi = local_heads(nh, group)
     out_h, lse_h = attn_fn(qh, kh, vh, [tuple(p) for p in head_params[lo:hi]], grid, tile, scale)

@@ -111,13 +111,14 @@ def test_against_the_definition(case):
 @pytest.mark.gpu
 def test_all_ways_of_handing_out_items():
     seen = set()
-    for grid, tile, heads, kind in (((8, 16, 16), (2, 8, 16), 2, "all"), ((3, 16, 48), (1, 16, 16), 40, "ragged"), ((4, 16, 16), (1, 16, 16), 30, "one")):
+    for grid, tile, heads, kind in (((8, 16, 16), (2, 8, 16), 2, "all"), ((3, 16, 48), (1, 16, 16), 40, "ragged"), ((4, 16, 16), (1, 16, 16), 30, "one"),
+                                    ((4, 32, 48), (1, 8, 16), 20, "ragged"), ((4, 31, 47), (1, 8, 16), 20, "ragged")):
         q, k, v = tensors(heads, math.prod(grid), 5)
         lists = random_lists(heads, blocks_of_tokens(grid, tile)[1], 6, kind)
         out, lse = B.psa_attn_fwd_lists(q, k, v, *pack(lists), grid, tile, SCALE)
         seen.add(B.psa_last_attn_launch()[1])
         check(out, lse, q, k, v, lists, grid, tile)
-    assert seen == {"ticket", "direct", "shared_direct"}
+    assert seen == {"ticket", "ticket_short", "direct", "shared_direct"}
 
 
 @pytest.mark.gpu
