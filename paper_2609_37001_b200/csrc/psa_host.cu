@@ -1545,6 +1545,7 @@ int psa_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, con
   const bool alike = prob->dtype == prob->out_dtype && (prob->n_batch == 1 || prob->stride_batch == prob->out_stride_batch) &&
                      (prob->n_heads == 1 || prob->stride_head == prob->out_stride_head) && (prob->n_tokens == 1 || prob->stride_token == prob->out_stride_token);
   if (!alike && (q == q_out || (k && k == k_out))) return PSA_ERR_INVALID_ARG;
+  if (k && (q_out == k_out || q_out == k || k_out == q)) return PSA_ERR_INVALID_ARG;
   a.in[0] = q; a.in[1] = k;
   a.out[0] = q_out; a.out[1] = k_out;
   a.weight[0] = q_weight; a.weight[1] = k_weight;

@@ -9,7 +9,7 @@
 // head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64); a block takes one or more tokens of
 // q and k, or (more than 16 heads) of one of them, all heads, so that a mean over all heads costs one read.  Blocks are persistent: a group's head is always the same, whose
 // weights, and sums for dw, stay in registers.  Two more warps of the block, the producers, copy the next tokens' rows into shared
-// memory (cp.async, kMaxStages sets at most) and compute cos and sin of their 64 pairs, once for all heads.
+// memory (cp.async, kMaxStages sets at most), and compute cos and sin of their 64 pairs, once for all heads.
 // The next bound is the issue of instructions (some 100 a row in a first version where every thread loaded its own rows and
 // computed its own angles, 65 % of the issue slots at 44 % of HBM): what is done for a token and not for a channel is left to the
 // producers, eight lanes a row instead of 16 halve what is spent on addresses, sums over lanes and roots, and arithmetic runs on
@@ -31,7 +31,7 @@ namespace {
 constexpr int kLanes = 8;         // lanes of a group
 constexpr int kPairs = kHeadDim / 2;
 constexpr int kMaxThreads = 512;   // besides the producers
-constexpr int kProducers = 64;     // threads: one a pair
+constexpr int kProducers = 64;     // threads: a warp that copies and one for angles
 constexpr int kMaxStages = 4;      // sets of rows in shared memory
 constexpr int kMaxGroups = kMaxThreads / kLanes;
 // Registers.  Forward 80, which are 24 warps an SM: with 64, 72 and 88, 24 heads of 115,456 tokens took 595, 559 and 587 us instead of
@@ -290,32 +290,33 @@ __device__ __forceinline__ Angle angle_of(const NormRopeArgs& a, int p) {
   const int axis = p < a.pairs[0] ? 0 : (p < a.pairs[1] ? 1 : (p < a.pairs[2] ? 2 : 3));
   return Angle{axis, axis < 3 ? a.step[axis] * a.turns[p] : 0.0, axis < 3 ? a.origin[axis] * a.turns[p] : 0.0};
 }
-// cos, sin and -sin of pair p of the block's tokens from `first` on into shared memory, [token][3][64]; 1 and 0 where nothing turns.
-__device__ __forceinline__ void fill_turns(const NormRopeArgs& a, const Angle& angle, int p, int first, float* turns) {
+// cos, sin and -sin of pairs p and p + 32 of the block's tokens from `first` on into shared memory, [token][3][64]; 1 and 0 where nothing
+// turns.
+__device__ __forceinline__ void fill_turns(const NormRopeArgs& a, const Angle* angle, int p, int first, float* turns) {
   for (int slot = 0; slot < a.slots; ++slot, turns += 3 * kPairs) {
     const int n = first + slot;
     if (n >= a.n_all || n < 0) break;
     int b, i;
     token_of(a, n, b, i);
-    const long long at = a.first_token + i;
-    float c = 1.f, s = 0.f;
-    if (angle.axis < 3 && at < a.n_video) {
-      const int j = (int)at, row = divide(j, a.by_w), t = divide(row, a.by_h);
-      const int index = angle.axis == 0 ? t : (angle.axis == 1 ? row - t * a.H : j - row * a.W);
-      const double quarters = __fma_rn(angle.per, (double)index, angle.at0);
+    const bool video = a.first_token + i < a.n_video;
+    const int j = video ? (int)(a.first_token + i) : 0, row = divide(j, a.by_w), t = divide(row, a.by_h);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int index = angle[k].axis == 0 ? t : (angle[k].axis == 1 ? row - t * a.H : j - row * a.W);
+      const double quarters = __fma_rn(angle[k].per, (double)index, angle[k].at0);
       // the nearest whole number of quarters, in the last bits of the sum (the host bounds positions far below 2^51)
       const double shifted = quarters + 6755399441055744.0;   // 1.5 * 2^52
       const int q = __double2loint(shifted);
       float x, y;
       quarter_turn((float)(quarters - (shifted - 6755399441055744.0)), x, y);
-      c = q & 1 ? y : x;
-      s = q & 1 ? x : y;
+      float c = q & 1 ? y : x, s = q & 1 ? x : y;
       c = __uint_as_float(__float_as_uint(c) ^ (uint32_t)((q + 1) & 2) << 30);
       s = __uint_as_float(__float_as_uint(s) ^ (uint32_t)(q & 2) << 30);
+      const bool turned = video && angle[k].axis < 3;
+      turns[p + 32 * k] = turned ? c : 1.f;
+      turns[kPairs + p + 32 * k] = turned ? s : 0.f;
+      turns[2 * kPairs + p + 32 * k] = turned ? -s : 0.f;
     }
-    turns[p] = c;
-    turns[kPairs + p] = s;
-    turns[2 * kPairs + p] = -s;
   }
 }
 
@@ -414,10 +415,10 @@ __device__ __forceinline__ void produce(const NormRopeArgs& a, const Shared& sh,
   const int x_bytes = x_too ? kHeadDim * (int)sizeof(T) : 0, token_bytes = a.n_heads * (x_bytes + (g_too ? kHeadDim * (int)sizeof(O) : 0));
   const int stages = a.stages;
   const uint32_t rows = (uint32_t)__cvta_generic_to_shared(sh.rows);
-  // 16-byte piece `me % pieces` of every (kProducers / pieces)-th head
+  // 16-byte piece `me % pieces` of every (32 / pieces)-th head
   auto copy_rows = [&](const auto* from, long long head_stride, uint32_t to) {
     using E = typename std::remove_cv<typename std::remove_pointer<decltype(from)>::type>::type;
-    constexpr int kPieces = kHeadDim * (int)sizeof(E) / 16, kStep = kProducers / kPieces;
+    constexpr int kPieces = kHeadDim * (int)sizeof(E) / 16, kStep = 32 / kPieces;
     const int piece = me % kPieces, h0 = me / kPieces;
     const E* p = from + h0 * head_stride + piece * (16 / (int)sizeof(E));
     to += (uint32_t)(h0 * kHeadDim * (int)sizeof(E) + piece * 16);
@@ -444,30 +445,34 @@ __device__ __forceinline__ void produce(const NormRopeArgs& a, const Shared& sh,
   };
   // first tokens of the sets to be copied, and computed with; a sum that passes 2^31 is the end, too
   auto after = [&](int first) -> int { return a.n_all - first > stride ? first + stride : a.n_all; };
-  const Angle angle = angle_of(a, me);
-  int first = (int)blockIdx.x * a.slots, ahead = first, stage = 0;
+  int first = (int)blockIdx.x * a.slots;
+  if (me >= 32) {   // the second warp: angles, those of the next tokens while these are worked on
+    const int p = me - 32;
+    const Angle angle[2] = {angle_of(a, p), angle_of(a, p + 32)};
+    fill_turns(a, angle, p, first, sh.turns);
+    for (int it = 0; first < a.n_all; ++it) {
+      block_barrier();
+      if (stages == 1) block_barrier();
+      first = after(first);
+      if (first < a.n_all) fill_turns(a, angle, p, first, sh.turns + ((it + 1) & 1) * 3 * a.slots * kPairs);
+    }
+    return;
+  }
+  int ahead = first, stage = 0;
   const int depth = stages > 1 ? stages - 1 : 1;   // sets in flight
   for (int k = 0; k < depth; ++k, ahead = after(ahead)) issue(ahead, k);
-  fill_turns(a, angle, me, first, sh.turns);
   copies_wait(depth - 1);
-  for (int it = 0; first < a.n_all; ++it) {
-    block_barrier();   // set `it` is there, and nobody reads the one before any more
-    const int next = after(first);
-    float* turns = sh.turns + ((it + 1) & 1) * 3 * a.slots * kPairs;
+  for (; first < a.n_all; first = after(first)) {
+    block_barrier();   // the set is there, and nobody reads the one before any more
     if (stages > 1) {
       issue(ahead, stage == 0 ? stages - 1 : stage - 1);
-      ahead = after(ahead);
       stage = stage + 1 == stages ? 0 : stage + 1;
-      if (next < a.n_all) fill_turns(a, angle, me, next, turns);
-      copies_wait(depth - 1);
     } else {
-      block_barrier();   // set `it` has been read
+      block_barrier();   // it has been read
       issue(ahead, 0);
-      ahead = after(ahead);
-      if (next < a.n_all) fill_turns(a, angle, me, next, turns);
-      copies_wait(0);
     }
-    first = next;
+    ahead = after(ahead);
+    copies_wait(depth - 1);
   }
   copies_wait(0);
 }

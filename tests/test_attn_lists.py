@@ -89,6 +89,7 @@ CASES = [
     ((3, 16, 48), (1, 16, 16), 40, "ragged", None, 130, "head"),  # more items than run at once
     ((6, 32, 33), (1, 32, 4), 20, "ragged", None, 0, "head"),
     ((11, 30, 52), (1, 30, 8), 3, "even", 77, 0, "head"),         # every block of long lists
+    ((5, 32, 48), (1, 16, 16), 5, "all", None, 0, "head"),        # two CTAs an item, more of them than run at once
 ]
 
 

@@ -325,7 +325,7 @@ REFUSED = [
     (dict(step=(1, math.inf, 1)), INVALID), (dict(q=None), INVALID), (dict(k=None), INVALID), (dict(k_out=None), INVALID), (dict(q=4104), INVALID),
     (dict(q_out=16392), INVALID), (dict(qw=65540), INVALID), (dict(stride=(0, 512, 132)), INVALID), (dict(stride=(0, 512, 0)), INVALID),
     (dict(stride=(0, 0, 128)), INVALID), (dict(n_batch=2), INVALID), (dict(out_stride=(0, 508, 128)), INVALID),
-    (dict(q_out=4096, out_stride=(0, 1024, 128)), INVALID), (dict(k_out=8192, dtype=2), INVALID), (dict(k=None, k_out=None), INVALID),
+    (dict(k_out=16384), INVALID), (dict(k_out=4096), INVALID), (dict(q_out=8192), INVALID), (dict(q_out=4096, out_stride=(0, 1024, 128)), INVALID), (dict(k_out=8192, dtype=2), INVALID), (dict(k=None, k_out=None), INVALID),
 ]
 
 
