@@ -6,9 +6,9 @@
 // g = R(-angles) dy, h = w * g, s = mean(h * x):  dx = r * (h - x * r^2 * s),  dw = sum of g * x * r.
 //
 // Bound by HBM: forward moves each value in and out once, the gradient x and dy in and dx out.  A group of eight lanes takes one
-// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64); a block takes one or more tokens of
-// q and k, or (more than 16 heads) of one of them, all heads, so that a mean over all heads costs one read.  Blocks are persistent: a group's head is always the same, whose
-// weights, and sums for dw, stay in registers.  Two more warps of the block, the producers, copy the next tokens' rows into shared
+// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64, backward 56); a block takes one or more tokens of
+// q and k, or (more than 16 heads, backward 8) of one of them, all heads, so that a mean over all heads costs one read.  Blocks
+// are persistent: a group's head is always the same, whose weights, and sums for dw, stay in registers.  Two more warps of the block, the producers, copy the next tokens' rows into shared
 // memory (cp.async, kMaxStages sets at most), and compute cos and sin of their 64 pairs, once for all heads.
 // The next bound is the issue of instructions (some 100 a row in a first version where every thread loaded its own rows and
 // computed its own angles, 65 % of the issue slots at 44 % of HBM): what is done for a token and not for a channel is left to the
@@ -33,14 +33,15 @@ constexpr int kPairs = kHeadDim / 2;
 constexpr int kMaxThreads = 512;   // besides the producers
 constexpr int kProducers = 64;     // threads: a warp that copies and one for angles
 constexpr int kMaxStages = 4;      // sets of rows in shared memory
-constexpr int kMaxGroups = kMaxThreads / kLanes;
+constexpr int kMaxGroups = kMaxThreads / kLanes, kMaxBwdGroups = (16 * 32 - kProducers) / kLanes;   // of one row each
 // Registers.  Forward 80, which are 24 warps an SM: with 64, 72 and 88, 24 heads of 115,456 tokens took 595, 559 and 587 us instead of
-// 520.  The gradient's sums, weights, x and dy want 104: 40 heads of 75,600 tokens with the norm over all heads take 1.01 ms as one
-// block an SM, and 1.17 with 80 registers and two.  (96 where a block of kMaxThreads + kProducers threads has to start.)
-constexpr int kRegs = 80, kBwdRegs = 104;
-// Threads of a block besides the producers, at most: with q and k, with several tokens.  (The producers are kept as busy by one
-// token as by one of few heads.)
-constexpr int kBlockThreads = 256, kSmallThreads = 64;
+// 520.  The gradient's sums, weights, x and dy want 128, which are 16 warps: 40 heads of 75,600 tokens with the norm over all heads
+// take 939 us, and with 80, 96 and 112 registers 1,249, 1,017 and 972.  (Two rows a group: 96, so that kMaxThreads + kProducers
+// threads start.)
+constexpr int kRegs = 80, kBwdRegs = 128, kTwoRowsRegs = 96;
+// Threads of a block besides the producers, at most: with q and k (forward and backward), with several tokens.  (A token of few heads
+// keeps the producers as busy as one of many.  12 heads of 32,760 tokens backward: 120 us with blocks of one tensor, 126 with both.)
+constexpr int kBothThreads = 256, kBothBwdThreads = 128, kSmallThreads = 64;
 
 // ------------------------------------------------------------------------------------------------ packed pairs
 typedef unsigned long long f2;    // two fp32 values, one instruction for both
@@ -479,7 +480,7 @@ __device__ __forceinline__ void produce(const NormRopeArgs& a, const Shared& sh,
 
 // ------------------------------------------------------------------------------------------------ forward
 template <class T, class O, int kNorm, bool kHalves, int kRows>
-__global__ void __maxnreg__(kRows == 1 ? kRegs : 96)
+__global__ void __maxnreg__(kRows == 1 ? kRegs : kTwoRowsRegs)
 norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
   extern __shared__ __align__(16) uint8_t sm[];
   const Shared sh = carve(a, sm);
@@ -549,7 +550,7 @@ norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
 // ------------------------------------------------------------------------------------------------ gradient
 // Like the forward pass.  Every block leaves one partial sum per weight, which norm_rope_dw_kernel adds in a fixed order.
 template <class T, class O, int kNorm, bool kHalves, int kRows>
-__global__ void __maxnreg__(kRows == 1 ? kBwdRegs : 96)
+__global__ void __maxnreg__(kRows == 1 ? kBwdRegs : kTwoRowsRegs)
 norm_rope_bwd_kernel(const __grid_constant__ NormRopeArgs a) {
   constexpr bool kHasNorm = kNorm != PSA_NORM_NONE;
   extern __shared__ __align__(16) uint8_t sm[];
@@ -725,7 +726,7 @@ cudaError_t launch_rows(NormRopeArgs& a, bool backward, int threads, int blocks,
   // as many sets of rows as fit, beside as many blocks as there are registers for
   const int bytes = a.slots * a.tensors * a.n_heads * kHeadDim * (int)(backward ? (kNorm != PSA_NORM_NONE ? sizeof(T) : 0) + sizeof(O) : sizeof(T));
   const size_t sums = backward ? (size_t)((threads - kProducers) / kLanes) * kHeadDim * sizeof(float) : 0;
-  const size_t share = kMaxSmemBytes / (65536 / ((backward ? kBwdRegs : kRegs) * threads)) - 1024;
+  const size_t share = kMaxSmemBytes / (65536 / ((kRows > 1 ? kTwoRowsRegs : backward ? kBwdRegs : kRegs) * threads)) - 1024;
   for (a.stages = kMaxStages; a.stages > 2 && shared_bytes(a.slots, bytes, a.stages) > share; --a.stages) {}
   while (a.stages > 1 && shared_bytes(a.slots, bytes, a.stages) > kMaxSmemBytes) --a.stages;
   const size_t rows = shared_bytes(a.slots, bytes, a.stages), smem = rows > sums ? rows : sums;
@@ -764,8 +765,8 @@ cudaError_t launch_norm(NormRopeArgs& a, int norm, bool halves, bool backward, i
 cudaError_t launch_norm_rope(NormRopeArgs& a, const psa_qk& prob, bool halves, bool backward, int n_sms, float* q_dw, float* k_dw, cudaStream_t st,
                              int* launches) {
   // Groups a token: one a head, or one for two.  Tokens a block: blocks of some 256 threads, whole warps.
-  a.parts = a.n_heads <= kMaxGroups ? a.n_heads : (a.n_heads + 1) / 2;
-  a.tensors = a.out[1] && 2 * a.parts * kLanes <= kBlockThreads ? 2 : 1;
+  a.parts = a.n_heads <= (backward ? kMaxBwdGroups : kMaxGroups) ? a.n_heads : (a.n_heads + 1) / 2;
+  a.tensors = a.out[1] && 2 * a.parts * kLanes <= (backward ? kBothBwdThreads : kBothThreads) ? 2 : 1;
   a.slots = kSmallThreads / (a.tensors * a.parts * kLanes);
   if (a.slots < 1) a.slots = 1;
   const int threads = ((a.slots * a.tensors * a.parts * kLanes + 31) & ~31) + kProducers, blocks = (int)(((long long)a.n_all + a.slots - 1) / a.slots);

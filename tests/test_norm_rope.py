@@ -97,6 +97,10 @@ CASES = [
     (torch.bfloat16, torch.bfloat16, 7, 2, (3, 4, 5), 20, (37, 41), "head", "shared", WIDE_SPACE, "interleaved", "fused", (0, 0, 0), (1, 1, 1)),
     (torch.float32, torch.float32, 2, 0, (5, 20, 31), 0, (1000, 1), "none", None, (128, 0, 0), "interleaved", "head", (1e6, 0, 0), (1, 1, 1)),
     (torch.bfloat16, torch.bfloat16, 24, 0, (5, 20, 31), 0, None, "head", "shared", (0, 0, 0), "halves", "head", (0, 0, 0), (1, 1, 1)),
+    (torch.bfloat16, torch.bfloat16, 56, 0, (2, 4, 41), 0, None, "token", "heads", WIDE_TIME, "interleaved", "head", (0, 0, 0), (1, 1, 1)),
+    (torch.float32, torch.float32, 57, 0, (2, 4, 41), 0, None, "token", "heads", WIDE_SPACE, "halves", "head", (0, 0, 0), (1, 1, 1)),
+    (torch.float16, torch.float16, 64, 2, (2, 4, 21), 1, None, "head", "shared", WIDE_TIME, "interleaved", "token", (0, 0, 0), (1, 1, 1)),
+    (torch.bfloat16, torch.bfloat16, 65, 0, (2, 4, 41), 0, None, "token", "heads", WIDE_TIME, "interleaved", "head", (0, 0, 0), (1, 1, 1)),
     (torch.bfloat16, torch.bfloat16, 3, 3000, (1, 1, 2), 0, (1, 1), "head", "heads", WIDE_TIME, "interleaved", "token", (0, 0, 0), (1, 1, 1)),
     (torch.bfloat16, torch.bfloat16, 20, 700, (1, 1, 3), 0, None, "token", "shared", WIDE_TIME, "interleaved", "head", (0, 0, 0), (1, 1, 1)),
     (torch.float32, torch.float32, 128, 0, (1, 13, 31), 5, None, "token", "heads", WIDE_TIME, "interleaved", "head", (0, 0, 0), (1, 1, 1)),
