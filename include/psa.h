@@ -261,8 +261,9 @@ int psa_search_select_at_sparsity(const float* losses, const float* sparsity, in
  * psa_qk_norm_rope_bwd: from the gradients dq_out, dk_out of the outputs (out_dtype, out_stride_*) those of q and k (dtype,
  * grad_stride_*; must not overlap anything else) and of the weights (device fp32 [weight_heads][128], sums over all tokens;
  * both or neither NULL, and NULL for PSA_NORM_NONE).  q and k are the forward call's (for PSA_NORM_NONE not read, may be NULL).
- * scratch: device, 16-byte aligned, psa_qk_norm_rope_bwd_scratch_bytes(prob) bytes, needed with weight gradients only.  Sums run
- * in a fixed order: a call repeated gives the same bits. */
+ * scratch: device, 16-byte aligned, psa_qk_norm_rope_bwd_scratch_bytes(prob) bytes, needed with weight gradients only; calls that may
+ * overlap on the GPU need one each.  Sums run in a fixed order: a call repeated gives the same bits.
+ * Neither call allocates anything; make the first one on a device before any stream capture begins. */
 typedef enum { PSA_BF16 = 0, PSA_FP16 = 1, PSA_FP32 = 2 } psa_dtype;
 typedef enum { PSA_NORM_NONE = 0, PSA_NORM_HEAD = 1, PSA_NORM_TOKEN = 2 } psa_norm;
 typedef enum { PSA_PAIRS_INTERLEAVED = 0, PSA_PAIRS_HALVES = 1 } psa_pairs;
@@ -295,7 +296,7 @@ int psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q, 
  * on it left behind: PSA_OK, or PSA_ERR_TIMEOUT if a bounded wait inside the kernel
  * expired (outputs are then undefined); also what a replay of a call captured in a CUDA graph
  * reported since the last query.  *detail (optional, host) receives a
- * diagnostic code naming the wait that gave up. */
+ * diagnostic code naming the wait that gave up.  psa_attn_fwd_lists reports here, too. */
 int psa_last_device_status(int32_t* detail);
 
 /* Self-test of the bounded device-side waits (no counterpart in the paper): launches a
@@ -320,7 +321,7 @@ typedef enum {
   PSA_LAUNCH_TICKET = 0,         /* persistent CTAs draw planned items                      */
   PSA_LAUNCH_DIRECT = 1,         /* every item runs at once, nothing is planned             */
   PSA_LAUNCH_SHARED = 2,         /* CTAs share planned items                                */
-  PSA_LAUNCH_SHARED_DIRECT = 3,  /* CTAs share items that all run at once                   */
+  PSA_LAUNCH_SHARED_DIRECT = 3,  /* CTAs share items that all run at once (over lists: of any number, in order) */
   PSA_LAUNCH_TICKET_EDGE = 4,    /* as 0, some blocks having slabs without any token        */
   PSA_LAUNCH_TICKET_SHORT = 5    /* as 0, few key slabs per item, blocks of one slab        */
 } psa_launch_mode;

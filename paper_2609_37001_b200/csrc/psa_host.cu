@@ -1123,8 +1123,9 @@ int psa_attn_fwd_lists(const void* q, const void* k, const void* v, void* out, f
   int* status;
   if ((rc = device_info(&dev, &ws)) != PSA_OK || (rc = init_attn(ws)) != PSA_OK || (rc = lists_status(dev, &status)) != PSA_OK) return rc;
   // The lists' lengths are in device memory: an average row is taken for the choice of CTAs per item.
-  const std::vector<long long> weights((size_t)prob->n_heads, n_entries / prob->n_heads);
-  const int cluster = share_items(*ws, g, weights.data(), prob->n_heads).cluster;
+  long long weights[kMaxHeads];
+  for (long long& w : weights) w = n_entries / prob->n_heads;
+  const int cluster = share_items(*ws, g, weights, prob->n_heads < kMaxHeads ? prob->n_heads : kMaxHeads).cluster;
   ws->last_call = next_call_id(st);
   ws->last_lists = true;
   const Layout lay = {prob->stride_head, prob->stride_token, prob->stride_head, prob->stride_token, false};
@@ -1148,7 +1149,7 @@ int psa_attn_fwd_lists(const void* q, const void* k, const void* v, void* out, f
     prm.counter = static_cast<int*>(scratch);
     // items shared by CTAs are taken in order, whatever their number
     const bool direct = cluster > 1 || runs_at_once(*ws, prm.n_items, cluster);
-    if (launch_lists(tm, prm, g, weights.data(), *ws, cluster, direct, st) != cudaSuccess) return PSA_ERR_CUDA;
+    if (launch_lists(tm, prm, g, weights, *ws, cluster, direct, st) != cudaSuccess) return PSA_ERR_CUDA;
   }
   return PSA_OK;
 }

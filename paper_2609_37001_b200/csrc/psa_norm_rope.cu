@@ -6,14 +6,16 @@
 // g = R(-angles) dy, h = w * g, s = mean(h * x):  dx = r * (h - x * r^2 * s),  dw = sum of g * x * r.
 //
 // Bound by HBM: forward moves each value in and out once, the gradient x and dy in and dx out.  A group of eight lanes takes one
-// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64, backward 56); a block takes one or more tokens of
-// q and k, or (more than 16 heads, backward 8) of one of them, all heads, so that a mean over all heads costs one read.  Blocks
-// are persistent: a group's head is always the same, whose weights, and sums for dw, stay in registers.  Two more warps of the block, the producers, copy the next tokens' rows into shared
-// memory (cp.async, kMaxStages sets at most), and compute cos and sin of their 64 pairs, once for all heads.
-// The next bound is the issue of instructions (some 100 a row in a first version where every thread loaded its own rows and
-// computed its own angles, 65 % of the issue slots at 44 % of HBM): what is done for a token and not for a channel is left to the
-// producers, eight lanes a row instead of 16 halve what is spent on addresses, sums over lanes and roots, and arithmetic runs on
-// packed pairs of 32-bit values.
+// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64, backward 56); a block takes one or more
+// tokens of q and k, or (more than 16 heads, backward 8) of one of them, all heads, so that a mean over all heads costs one read.
+// Blocks are persistent: a group's head is always the same, whose weights, and sums for dw, stay in registers.  Two more warps of
+// the block, the producers, copy the next tokens' rows into shared memory (cp.async, kMaxStages sets at most), and compute cos and
+// sin of their 64 pairs, once for all heads.
+// The next bounds are the waits between a token's steps (sums of lanes, the barrier, the sum over heads: with the mean over all heads
+// 12 heads of 2 x 32,760 tokens reach 0.71 to 0.74 of the copy rate forward, 40 of 75,600 0.73 to 0.76 backward), and the issue of
+// instructions (some 100 a row in a first version where every thread loaded its own rows and computed its own angles, 65 % of the
+// issue slots at 44 % of HBM): what is done for a token and not for a channel is left to the producers, eight lanes a row instead of
+// 16 halve what is spent on addresses, sums over lanes and roots, and arithmetic runs on packed pairs of 32-bit values.
 //
 // Angles: position times frequency in 64 bits, as only the fraction of a turn counts and positions may be far; the distance
 // to the nearest quarter turn then in 32 bits.  Sums, norms and rotations are in 32 bits, rounded once.
@@ -34,8 +36,8 @@ constexpr int kMaxThreads = 512;   // besides the producers
 constexpr int kProducers = 64;     // threads: a warp that copies and one for angles
 constexpr int kMaxStages = 4;      // sets of rows in shared memory
 constexpr int kMaxGroups = kMaxThreads / kLanes, kMaxBwdGroups = (16 * 32 - kProducers) / kLanes;   // of one row each
-// Registers.  Forward 80, which are 24 warps an SM: with 64, 72 and 88, 24 heads of 115,456 tokens took 595, 559 and 587 us instead of
-// 520.  The gradient's sums, weights, x and dy want 128, which are 16 warps: 40 heads of 75,600 tokens with the norm over all heads
+// Registers.  Forward 80, which are 24 warps an SM: with 64 and 72, 24 heads of 115,456 tokens take 606 and 522 us instead of 486 (5.8
+// TB/s, 0.89 of what a copy reaches).  The gradient's sums, weights, x and dy want 128, which are 16 warps: 40 heads of 75,600 tokens with the norm over all heads
 // take 939 us, and with 80, 96 and 112 registers 1,249, 1,017 and 972.  (Two rows a group: 96, so that kMaxThreads + kProducers
 // threads start.)
 constexpr int kRegs = 80, kBwdRegs = 128, kTwoRowsRegs = 96;
