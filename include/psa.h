@@ -199,7 +199,8 @@ int psa_select_blocks(const void* q, const void* k, const psa_problem* prob, int
  *   row_ptr   device int32 [n_heads*NB + 1]: query block i of head h attends key blocks col_idx[row_ptr[r]] ..
  *             col_idx[row_ptr[r + 1] - 1], r = h*NB + i, ascending; none: out = 0 and lse = -inf for its tokens (with text:
  *             the text alone)
- *   col_idx   device int32 [n_entries] (may be NULL if n_entries is 0)
+ *   col_idx   device int32 [n_entries] (may be NULL if n_entries is 0); n_entries / (n_heads*NB) is taken for the length of an
+ *             average list where the launch is chosen, so it should be the number of entries in use
  *   n_text    as for psa_attn_fwd_joint: text keys are attended by every query, text queries attend every key
  *   scratch   device, 16-byte aligned, psa_attn_fwd_lists_scratch_bytes(...) bytes; calls that may overlap on the GPU, and graphs
  *             that may, need one each

@@ -1474,8 +1474,9 @@ int psa_attn_fwd_host(const void* q, const void* k, const void* v, void* out, fl
 static int norm_rope_args(const psa_qk* prob, const psa_rope* rope, int T, int H, int W, NormRopeArgs* a, bool* nothing) {
   if (!prob || !rope || T < 1 || H < 1 || W < 1 || prob->n_batch < 1 || prob->n_heads < 1) return PSA_ERR_INVALID_ARG;
   if (prob->head_dim != kHeadDim || prob->n_heads > kMaxHeads) return PSA_ERR_UNSUPPORTED;
-  const long long L = (long long)T * H * W, lim = 1ll << 31;
-  if ((long long)T * H >= lim || L >= lim) return PSA_ERR_INVALID_ARG;
+  const long long lim = 1ll << 31;
+  if ((long long)T * H >= lim || (long long)T * H * W >= lim) return PSA_ERR_INVALID_ARG;
+  const long long L = (long long)T * H * W;
   if (prob->n_text < 0 || prob->n_text >= lim || prob->first_token < 0 || prob->n_tokens < 0 || prob->n_tokens >= lim ||
       prob->first_token >= lim * 2 || prob->first_token + prob->n_tokens > L + prob->n_text)
     return PSA_ERR_INVALID_ARG;

@@ -34,7 +34,8 @@ constexpr int kLanes = 8;         // lanes of a group
 constexpr int kPairs = kHeadDim / 2;
 constexpr int kMaxThreads = 512;   // besides the producers
 constexpr int kProducers = 64;     // threads: a warp that copies and one for angles
-constexpr int kMaxStages = 4;      // sets of rows in shared memory
+// Sets of rows in shared memory.  24 heads of 115,456 tokens on one card, us with 2, 3 and 4 sets: 1,268, 529, 469; no less with 5 to 8.
+constexpr int kMaxStages = 4;
 constexpr int kMaxGroups = kMaxThreads / kLanes, kMaxBwdGroups = (16 * 32 - kProducers) / kLanes;   // of one row each
 // Registers.  Forward 80, which are 24 warps an SM: with 64 and 72, 24 heads of 115,456 tokens take 606 and 522 us instead of 486 (5.8
 // TB/s, 0.89 of what a copy reaches).  The gradient's sums, weights, x and dy want 128, which are 16 warps: 40 heads of 75,600 tokens with the norm over all heads
