@@ -12,7 +12,7 @@
 // the block, the producers, copy the next tokens' rows into shared memory (cp.async, kMaxStages sets at most), and compute cos and
 // sin of their 64 pairs, once for all heads.
 // The next bounds are the waits between a token's steps (sums of lanes, the barrier, the sum over heads: with the mean over all heads
-// 12 heads of 2 x 32,760 tokens reach 0.71 to 0.74 of the copy rate forward, 40 of 75,600 0.73 to 0.76 backward), and the issue of
+// 12 heads of 2 x 32,760 tokens reach 0.70 to 0.75 of the copy rate forward, 40 of 75,600 0.70 to 0.76 backward), and the issue of
 // instructions (some 100 a row in a first version where every thread loaded its own rows and computed its own angles, 65 % of the
 // issue slots at 44 % of HBM): what is done for a token and not for a channel is left to the producers, eight lanes a row instead of
 // 16 halve what is spent on addresses, sums over lanes and roots, and arithmetic runs on packed pairs of 32-bit values.
