@@ -71,7 +71,8 @@ def psa_attn_fwd_ulysses(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head
 
     ``norm_rope``: options of ``binding.psa_qk_norm_rope`` (dims, norm, weights of all heads, ...).  With it q and k
     are normed and rotated here first, where a rank still holds all heads of its tokens, which a mean over all
-    heads needs; the options do not name the tokens, which are this rank's.
+    heads needs; the options name neither the tokens, which are this rank's, nor a stream: the exchanges read the
+    normed q and k on the current one.
 
     ``attn_fn(q, k, v, params, grid, tile, scale) -> (out, lse)`` defaults to ``binding.psa_attn_fwd``,
     ``norm_rope_fn`` to ``binding.psa_qk_norm_rope``; the CPU tests pass their own."""
@@ -89,6 +90,8 @@ def psa_attn_fwd_ulysses(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head
     if norm_rope is not None:
         if "first_token" in norm_rope or "out" in norm_rope or norm_rope.get("n_text", 0):
             raise ValueError("norm_rope: this rank's video tokens, into new tensors")
+        if norm_rope.get("stream") is not None:
+            raise ValueError("norm_rope: on the current stream, as what follows it")
         rank = dist.get_rank(group) if P > 1 else 0
         q, k = norm_rope_fn(q, k, grid, first_token=rank * q.shape[1], **norm_rope)
     qh, kh, vh = (seq_to_head_shards(t, group) for t in (q, k, v))
