@@ -448,6 +448,19 @@ def _strides4(t: torch.Tensor) -> Tuple[int, int, int]:
     return (0, st[0], st[1]) if len(st) == 3 else st[:3]
 
 
+def _new_like(x: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """A new tensor of x's shape and strides, gaps included, as attention asks of q, k and v together (v may still lie in the projection that
+    x is a view of).  Without gaps where elements of x share memory, which those of an output must not."""
+    st = x.stride()
+    span = 1
+    for s, n in sorted(zip(st, x.shape)):
+        if n > 1:
+            if s < span:
+                return torch.empty_like(x, dtype=dtype)
+            span += s * (n - 1)
+    return x.new_empty_strided(x.shape, st, dtype=dtype)
+
+
 def _norm_rope_call(first: torch.Tensor, out: torch.Tensor, grad: Optional[torch.Tensor], dtype: torch.dtype, q_weight, k_weight, two: bool,
                     dims, theta, norm, eps, pairs, origin, step, n_text, first_token) -> Tuple[bytes, bytes, int]:
     """psa_qk and psa_rope of a call as packed bytes, and the heads that the weights are of (0: no weights)."""
@@ -513,13 +526,14 @@ def psa_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], grid: Sequence[
     of T*H*W video tokens and ``n_text`` text tokens, which are normed and not rotated.
     ``dims``: channels that turn with the frame, the row and the column.  ``norm``: "head", "token" (over all heads) or "none"; weights
     [128] or [heads, 128].  Positions are ``origin + step * index``.  ``out``: (q_out, k_out), which may be (q, k); by default new
-    tensors of q's layout without gaps, of ``out_dtype`` (q's type, or bf16).  Returns (q_out, k_out)."""
+    tensors with q's strides, as attention's ``out`` (q, k and v of one projection still share strides then), of ``out_dtype`` (q's
+    type, or bf16).  Returns (q_out, k_out)."""
     two = k is not None
     if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
         raise ValueError("q and k must share shape, strides and type")
     if out is None:
-        q_out = torch.empty_like(q, dtype=out_dtype)
-        k_out = torch.empty_like(k, dtype=out_dtype) if two else None
+        q_out = _new_like(q, out_dtype)
+        k_out = _new_like(k, out_dtype) if two else None
         _used_on(stream, q_out, k_out)
     else:
         q_out, k_out = out
