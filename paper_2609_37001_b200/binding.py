@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+from contextlib import nullcontext
 from itertools import chain
 from typing import List, Optional, Sequence, Tuple
 
@@ -184,6 +185,26 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+_CURRENT = nullcontext()
+
+
+def _memory_of(stream: Optional[torch.cuda.Stream]):
+    """Context for the allocations of a call on `stream`: memory of that stream.  (Memory of the current stream may have been dropped while
+    kernels there still use it, behind which nothing orders the call's.)"""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
+
+
+def _used_here(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> None:
+    """Tensors allocated for a call on `stream` and returned: the current stream may read them until they are dropped, before `stream` gets
+    their memory again."""
+    if stream is not None:
+        here = torch.cuda.current_stream()
+        if stream != here:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(here)
+
+
 def _require_cuda(*tensors: torch.Tensor) -> None:
     for t in tensors:
         if not t.is_cuda:
@@ -208,9 +229,11 @@ def psa_mask_build(head_params, grid: Sequence[int], tile: Sequence[int], device
     T, H, W = map(int, grid)
     if out is None:
         nb, nnz = psa_mask_sizes(head_params, grid, tile)
-        mask = torch.empty((nh, nb, nb), dtype=torch.uint8, device=device)
-        row_ptr = torch.empty(nh * nb + 1, dtype=torch.int32, device=device)
-        col_idx = torch.empty(max(nnz, 1), dtype=torch.int32, device=device)
+        with _memory_of(stream):
+            mask = torch.empty((nh, nb, nb), dtype=torch.uint8, device=device)
+            row_ptr = torch.empty(nh * nb + 1, dtype=torch.int32, device=device)
+            col_idx = torch.empty(max(nnz, 1), dtype=torch.int32, device=device)
+        _used_here(stream, mask, row_ptr, col_idx)
     else:
         mask, row_ptr, col_idx = out
         nnz = None
@@ -224,7 +247,7 @@ def psa_mask_build(head_params, grid: Sequence[int], tile: Sequence[int], device
     return mask, row_ptr, col_idx
 
 
-def _device_call(q, k, v, out, lse, lse_shape):
+def _device_call(q, k, v, out, lse, lse_shape, stream):
     """Checks the tensors of a device call and allocates the outputs that were not given.
     Returns (out, lse, q's strides)."""
     _require_cuda(q, k, v)
@@ -234,14 +257,17 @@ def _device_call(q, k, v, out, lse, lse_shape):
     st = q.stride()
     if st != k.stride() or st != v.stride() or st[-1] != 1:
         raise ValueError("q, k, v must share strides with a contiguous last dimension")
-    if out is None:
-        out = q.new_empty_strided(q.shape, st)
-    elif out.stride() != st:
+    if (out is not None and out.stride() != st) or (lse is not None and not lse.is_contiguous()):
         raise ValueError("out must share q's strides; lse must be contiguous")
-    if lse is None:
-        lse = q.new_empty(lse_shape, dtype=torch.float32)
-    elif not lse.is_contiguous():
-        raise ValueError("out must share q's strides; lse must be contiguous")
+    if out is None or lse is None:
+        mine = out, lse
+        with _memory_of(stream):
+            if out is None:
+                out = q.new_empty_strided(q.shape, st)
+            if lse is None:
+                lse = q.new_empty(lse_shape, dtype=torch.float32)
+        if stream is not None:
+            _used_here(stream, *(new for new, given in zip((out, lse), mine) if given is None))
     return out, lse, st
 
 
@@ -254,7 +280,7 @@ def psa_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head_params,
     T, H, W = map(int, grid)
     if L != T * H * W or k.shape != q.shape or v.shape != q.shape:
         raise ValueError("shape mismatch")
-    out, lse, st = _device_call(q, k, v, out, lse, (nh, L))
+    out, lse, st = _device_call(q, k, v, out, lse, (nh, L), stream)
     prob = _problem(nh, tile, scale, st[0], st[1], d)
     _check(lib().psa_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                               _params_array(head_params), prob, T, H, W, _stream_ptr(stream)),
@@ -272,7 +298,7 @@ def psa_attn_fwd_batched(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head
     T, H, W = map(int, grid)
     if L != T * H * W or k.shape != q.shape or v.shape != q.shape or len(head_params) != nh:
         raise ValueError("shape mismatch")
-    out, lse, st = _device_call(q, k, v, out, lse, (nb, nh, L))
+    out, lse, st = _device_call(q, k, v, out, lse, (nb, nh, L), stream)
     prob = _problem(nh, tile, scale, st[1], st[2], d)
     _check(lib().psa_attn_fwd_batched(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                       _params_array(head_params), prob, nb, st[0], T, H, W,
@@ -290,7 +316,7 @@ def psa_attn_fwd_joint(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head_p
     T, H, W = map(int, grid)
     if Lt != T * H * W + int(n_text) or k.shape != q.shape or v.shape != q.shape:
         raise ValueError("shape mismatch")
-    out, lse, st = _device_call(q, k, v, out, lse, (nh, Lt))
+    out, lse, st = _device_call(q, k, v, out, lse, (nh, Lt), stream)
     prob = _problem(nh, tile, scale, st[0], st[1], d)
     _check(lib().psa_attn_fwd_joint(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                     _params_array(head_params), prob, int(n_text), T, H, W,
@@ -369,11 +395,13 @@ def psa_search_losses(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, candida
         raise ValueError("q, k, v must share strides with a contiguous last dimension")
     n_cand = len(candidates)
     need = psa_search_scratch_bytes(n_cand, grid)
-    if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
-    if scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
+    if scratch is not None and (scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous()):
         raise ValueError("scratch too small")
-    losses = torch.empty(n_cand, dtype=torch.float32, device=q.device)
+    with _memory_of(stream):
+        if scratch is None:
+            scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        losses = torch.empty(n_cand, dtype=torch.float32, device=q.device)
+    _used_here(stream, losses)
     prob = _problem(1, tile, scale, 0, q.stride(0), d)
     _check(lib().psa_search_losses(q.data_ptr(), k.data_ptr(), v.data_ptr(), _params_array(candidates), n_cand,
                                    prob, T, H, W, scratch.data_ptr(), losses.data_ptr(),
@@ -423,14 +451,6 @@ def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
                     here = torch._C._cuda_getDevice()
                 if index != here:
                     raise ValueError("tensors must be on the current device")
-
-
-def _used_on(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> None:
-    """Memory allocated here on the current stream and used on `stream`."""
-    if stream is not None and stream != torch.cuda.current_stream():
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
 
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
@@ -532,9 +552,10 @@ def psa_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], grid: Sequence[
     if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
         raise ValueError("q and k must share shape, strides and type")
     if out is None:
-        q_out = _new_like(q, out_dtype)
-        k_out = _new_like(k, out_dtype) if two else None
-        _used_on(stream, q_out, k_out)
+        with _memory_of(stream):
+            q_out = _new_like(q, out_dtype)
+            k_out = _new_like(k, out_dtype) if two else None
+        _used_here(stream, q_out, k_out)
     else:
         q_out, k_out = out
         if q_out.shape != q.shape or (k_out is not None) != two or (out_dtype is not None and q_out.dtype != out_dtype):
@@ -568,17 +589,19 @@ def psa_qk_norm_rope_bwd(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q
             raise ValueError("q and k must be those of the outputs")
         if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
             raise ValueError("q and k must share shape, strides and type")
-    dq = torch.empty_like(like)
-    dk = torch.empty_like(like) if two else None
+    with _memory_of(stream):
+        dq = torch.empty_like(like)
+        dk = torch.empty_like(like) if two else None
     _on_current_device(dq_out, dk_out, q, k, q_weight, k_weight)
     prob, rope, weight_heads = _norm_rope_call(like, dq_out, dq, like.dtype, q_weight, k_weight, two, dims, theta, norm, eps, pairs, origin, step,
                                                n_text, first_token)
     dq_weight = dk_weight = scratch = None
     if weight_heads:
-        dq_weight = torch.empty(q_weight.shape, dtype=torch.float32, device=q.device)
-        dk_weight = torch.empty_like(dq_weight) if two else None
-        scratch = torch.empty(int(lib().psa_qk_norm_rope_bwd_scratch_bytes(prob)), dtype=torch.uint8, device=q.device)
-    _used_on(stream, dq, dk, dq_weight, dk_weight, scratch)
+        with _memory_of(stream):
+            dq_weight = torch.empty(q_weight.shape, dtype=torch.float32, device=q.device)
+            dk_weight = torch.empty_like(dq_weight) if two else None
+            scratch = torch.empty(int(lib().psa_qk_norm_rope_bwd_scratch_bytes(prob)), dtype=torch.uint8, device=q.device)
+    _used_here(stream, dq, dk, dq_weight, dk_weight)
     T, H, W = map(int, grid)
     _check(lib().psa_qk_norm_rope_bwd(dq_out.data_ptr(), _ptr(dk_out), _ptr(q), _ptr(k), dq.data_ptr(), _ptr(dk), _ptr(q_weight), _ptr(k_weight),
                                       _ptr(dq_weight), _ptr(dk_weight), prob, rope, T, H, W, _ptr(scratch), _stream_ptr(stream)),
@@ -621,19 +644,18 @@ def psa_select_blocks(q: torch.Tensor, k: torch.Tensor, grid: Sequence[int], til
         raise ValueError("keep: between 1 and the number of blocks, one for all heads or one each")
     prob = _problem(nh, tile, 1.0, st[0], st[1], d)
     need = _scratch_bytes("select", nh, grid, tile)
-    new = []
     if out is None:
-        out = (torch.empty(nh * nb + 1, dtype=torch.int32, device=q.device), torch.empty(sum(each) * nb, dtype=torch.int32, device=q.device))
-        new.extend(out)
+        with _memory_of(stream):
+            out = (torch.empty(nh * nb + 1, dtype=torch.int32, device=q.device), torch.empty(sum(each) * nb, dtype=torch.int32, device=q.device))
+        _used_here(stream, *out)
     elif any(x.dtype != torch.int32 or not x.is_contiguous() for x in out) or out[0].numel() != nh * nb + 1 or out[1].numel() < sum(each) * nb:
         raise ValueError("row_ptr (heads * blocks + 1 entries) and col_idx must be contiguous int32 tensors")
     row_ptr, col_idx = out
     if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
-        new.append(scratch)
+        with _memory_of(stream):
+            scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
     elif scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
         raise ValueError("scratch too small")
-    _used_on(stream, *new)
     _check(lib().psa_select_blocks(q.data_ptr(), k.data_ptr(), prob, T, H, W, struct.pack("%di" % nh, *each), 1 if keep_self else 0, row_ptr.data_ptr(),
                                    col_idx.data_ptr(), col_idx.numel(), scratch.data_ptr(), _stream_ptr(stream)), "psa_select_blocks")
     return row_ptr, col_idx
@@ -668,19 +690,16 @@ def psa_attn_fwd_lists(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_pt
     i32 = torch.int32
     if row_ptr.dtype != i32 or col_idx.dtype != i32 or not row_ptr.is_contiguous() or not col_idx.is_contiguous() or row_ptr.numel() != nh * nb + 1:
         raise ValueError("row_ptr (heads * blocks + 1 entries) and col_idx must be contiguous int32 tensors")
-    mine = (out, lse)
     if (out is not None and (out.shape != q.shape or out.dtype != q.dtype)) or (lse is not None and (tuple(lse.shape) != (nh, Lt) or lse.dtype != torch.float32)):
         raise ValueError("out must be like q, lse fp32 [heads, tokens]")
-    out, lse, st = _device_call(q, k, v, out, lse, (nh, Lt))
+    out, lse, st = _device_call(q, k, v, out, lse, (nh, Lt), stream)
     prob = _problem(nh, tile, scale, st[0], st[1], d)
     need = _scratch_bytes("lists", nh, grid, tile, n_text)
-    given = scratch
     if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        with _memory_of(stream):
+            scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
     elif scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
         raise ValueError("scratch too small")
-    if stream is not None:
-        _used_on(stream, *(t for t, m in zip((out, lse, scratch), (*mine, given)) if m is None))
     _check(lib().psa_attn_fwd_lists(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), row_ptr.data_ptr(), col_idx.data_ptr(),
                                     col_idx.numel(), prob, n_text, T, H, W, scratch.data_ptr(), _stream_ptr(stream)), "psa_attn_fwd_lists")
     return out, lse
