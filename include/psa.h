@@ -247,8 +247,9 @@ int psa_search_select_at_sparsity(const float* losses, const float* sparsity, in
  *   u = x * r * weight              weight: [128], or [n_heads][128]; NULL: 1
  *   the first dim_t / 2 pairs of channels turn with the token's frame, the next dim_h / 2 with its row, the next dim_w / 2 with
  *   its column, channels beyond dim_t + dim_h + dim_w = R not at all.  Pair j of an axis of d channels turns by
- *   (origin + step * index) * theta^(-2 j / d), computed in 64 bits.  Pair p is channels 2p and 2p + 1, or p and p + R / 2
- *   (PSA_PAIRS_HALVES; R a multiple of 16):  (a, b) -> (a cos - b sin, a sin + b cos).
+ *   (origin + step * index) * theta^(-2 j / d), computed in 64 bits (off by 2^-51 of |origin| + |step * index| times the frequency at
+ *   most).  Pair p is channels 2p and 2p + 1, or p and p + R / 2 (PSA_PAIRS_HALVES; R a multiple of 16):
+ *   (a, b) -> (a cos - b sin, a sin + b cos).
  * Tokens T*H*W .. T*H*W + n_text - 1 of the sequence (text) are normed and not rotated.  The tensors hold tokens first_token ..
  * first_token + n_tokens - 1 of the sequence, e.g. one rank's part (n_tokens 0: nothing happens).  Arithmetic in 32 bits, one
  * rounding at the end.
