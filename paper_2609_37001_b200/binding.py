@@ -2,7 +2,8 @@
 
 Every step of the path runs inside the CUDA library; torch is used for device memory
 and streams.  Importing this module without a built library, or calling it without a
-CUDA device, raises -- there is no CPU fallback.
+CUDA device, raises -- there is no CPU fallback.  Attention is forward only: its outputs carry no
+gradient.  Norm and rotation (psa_qk_norm_rope) have one.
 """
 from __future__ import annotations
 
@@ -14,6 +15,7 @@ from itertools import chain
 from typing import List, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpsa.so")
@@ -547,7 +549,14 @@ def psa_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], grid: Sequence[
     ``dims``: channels that turn with the frame, the row and the column.  ``norm``: "head", "token" (over all heads) or "none"; weights
     [128] or [heads, 128].  Positions are ``origin + step * index``.  ``out``: (q_out, k_out), which may be (q, k); by default new
     tensors with q's strides, as attention's ``out`` (q, k and v of one projection still share strides then), of ``out_dtype`` (q's
-    type, or bf16).  Returns (q_out, k_out)."""
+    type, or bf16).  Returns (q_out, k_out).
+
+    Where q, k or a weight requires a gradient, the new tensors have one, by psa_qk_norm_rope_bwd (first derivatives; into ``out`` the
+    call takes no part in autograd).  As everywhere in autograd, a backward pass is captured into a CUDA graph only while no graph of the same
+    leaves from outside the capture is alive."""
+    if out is None and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
+        how = dict(dims=dims, theta=theta, norm=norm, eps=eps, pairs=pairs, origin=origin, step=step, n_text=n_text, first_token=first_token, stream=stream)
+        return _NormRope.apply(q, k, q_weight, k_weight, grid, out_dtype, how)
     two = k is not None
     if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
         raise ValueError("q and k must share shape, strides and type")
@@ -607,6 +616,48 @@ def psa_qk_norm_rope_bwd(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], q
                                       _ptr(dq_weight), _ptr(dk_weight), prob, rope, T, H, W, _ptr(scratch), _stream_ptr(stream)),
            "psa_qk_norm_rope_bwd")
     return dq, dk, dq_weight, dk_weight
+
+
+def _as_it_lies(t: torch.Tensor) -> bool:
+    """Whether the kernels can read a tensor of [..., tokens, 128] as it lies in memory."""
+    st = t.stride()
+    return st[-1] == 1 and t.data_ptr() % 16 == 0 and all(n <= 1 or (s >= 128 and s % 8 == 0) for n, s in zip(t.shape[:-1], st[:-1]))
+
+
+class _NormRope(torch.autograd.Function):
+    """psa_qk_norm_rope and its gradient, psa_qk_norm_rope_bwd."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, grid, out_dtype, how):
+        q_out, k_out = psa_qk_norm_rope(q, k, grid, q_weight=q_weight, k_weight=k_weight, out_dtype=out_dtype, **how)
+        needed = how["norm"] != "none" or q.dtype != q_out.dtype   # (a rotation's gradient needs their type, if it is another one)
+        ctx.save_for_backward(*((q, k) if needed else (None, None)), q_weight, k_weight)
+        ctx.call = grid, how
+        return q_out, k_out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight = ctx.saved_tensors
+        grid, how = ctx.call
+        grads = [g for g in (dq_out, dk_out) if g is not None]
+        if not all(_as_it_lies(g) for g in grads) or grads[0].stride() != grads[-1].stride():   # (of a sum, say: one value for all)
+            grads = [g.clone(memory_format=torch.contiguous_format) for g in grads]
+        stream, here = how["stream"], None
+        if stream is not None:   # q and k are ready there, the gradients here
+            here = torch.cuda.current_stream()
+            stream.wait_stream(here)
+            for g in grads:
+                g.record_stream(stream)
+        dq, dk, dq_weight, dk_weight = psa_qk_norm_rope_bwd(grads[0], grads[1] if len(grads) > 1 else None, q, k, grid, q_weight=q_weight,
+                                                            k_weight=k_weight, **how)
+        if stream is not None:
+            here.wait_stream(stream)
+        if dq_weight is not None:
+            dq_weight = dq_weight.to(q_weight.dtype)
+        if dk_weight is not None:
+            dk_weight = dk_weight.to(k_weight.dtype)
+        return dq, dk, dq_weight, dk_weight, None, None, None
 
 
 def psa_select_scratch_bytes(n_heads: int, grid: Sequence[int], tile: Sequence[int]) -> int:

@@ -93,7 +93,8 @@ def psa_attn_fwd_ulysses(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, head
         if norm_rope.get("stream") is not None:
             raise ValueError("norm_rope: on the current stream, as what follows it")
         rank = dist.get_rank(group) if P > 1 else 0
-        q, k = norm_rope_fn(q, k, grid, first_token=rank * q.shape[1], **norm_rope)
+        with torch.no_grad():   # (attention is forward only)
+            q, k = norm_rope_fn(q, k, grid, first_token=rank * q.shape[1], **norm_rope)
     qh, kh, vh = (seq_to_head_shards(t, group) for t in (q, k, v))
     lo, hi = local_heads(nh, group)
     out_h, lse_h = attn_fn(qh, kh, vh, [tuple(p) for p in head_params[lo:hi]], grid, tile, scale)
