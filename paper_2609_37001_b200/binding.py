@@ -207,6 +207,13 @@ def _used_here(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Ten
                     t.record_stream(here)
 
 
+def _new_scratch(need: int, like: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+    with _memory_of(stream):
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+
+
 def _require_cuda(*tensors: torch.Tensor) -> None:
     for t in tensors:
         if not t.is_cuda:
@@ -259,17 +266,19 @@ def _device_call(q, k, v, out, lse, lse_shape, stream):
     st = q.stride()
     if st != k.stride() or st != v.stride() or st[-1] != 1:
         raise ValueError("q, k, v must share strides with a contiguous last dimension")
-    if (out is not None and out.stride() != st) or (lse is not None and not lse.is_contiguous()):
-        raise ValueError("out must share q's strides; lse must be contiguous")
-    if out is None or lse is None:
+    if stream is not None and (out is None or lse is None):
         mine = out, lse
         with _memory_of(stream):
-            if out is None:
-                out = q.new_empty_strided(q.shape, st)
-            if lse is None:
-                lse = q.new_empty(lse_shape, dtype=torch.float32)
-        if stream is not None:
-            _used_here(stream, *(new for new, given in zip((out, lse), mine) if given is None))
+            out, lse, _ = _device_call(q, k, v, out, lse, lse_shape, None)
+        _used_here(stream, *(new for new, given in zip((out, lse), mine) if given is None))
+    if out is None:
+        out = q.new_empty_strided(q.shape, st)
+    elif out.stride() != st:
+        raise ValueError("out must share q's strides; lse must be contiguous")
+    if lse is None:
+        lse = q.new_empty(lse_shape, dtype=torch.float32)
+    elif not lse.is_contiguous():
+        raise ValueError("out must share q's strides; lse must be contiguous")
     return out, lse, st
 
 
@@ -470,17 +479,22 @@ def _strides4(t: torch.Tensor) -> Tuple[int, int, int]:
     return (0, st[0], st[1]) if len(st) == 3 else st[:3]
 
 
-def _new_like(x: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
-    """A new tensor of x's shape and strides, gaps included, as attention asks of q, k and v together (v may still lie in the projection that
+def _new_outputs(x: torch.Tensor, dtype: Optional[torch.dtype], two: bool) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """New tensors of x's shape and strides, gaps included, as attention asks of q, k and v together (v may still lie in the projection that
     x is a view of).  Without gaps where elements of x share memory, which those of an output must not."""
+    y = torch.empty_like(x, dtype=dtype)
     st = x.stride()
-    span = 1
-    for s, n in sorted(zip(st, x.shape)):
-        if n > 1:
-            if s < span:
-                return torch.empty_like(x, dtype=dtype)
-            span += s * (n - 1)
-    return x.new_empty_strided(x.shape, st, dtype=dtype)
+    if y.stride() != st:   # (x has either)
+        span = 1
+        for s, n in sorted(zip(st, x.shape)):
+            if n > 1:
+                if s < span:
+                    break
+                span += s * (n - 1)
+        else:
+            y = x.new_empty_strided(x.shape, st, dtype=dtype)
+            return y, y.new_empty_strided(x.shape, st) if two else None
+    return y, torch.empty_like(y) if two else None
 
 
 def _norm_rope_call(first: torch.Tensor, out: torch.Tensor, grad: Optional[torch.Tensor], dtype: torch.dtype, q_weight, k_weight, two: bool,
@@ -554,17 +568,21 @@ def psa_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], grid: Sequence[
     Where q, k or a weight requires a gradient, the new tensors have one, by psa_qk_norm_rope_bwd (first derivatives; into ``out`` the
     call takes no part in autograd).  As everywhere in autograd, a backward pass is captured into a CUDA graph only while no graph of the same
     leaves from outside the capture is alive."""
-    if out is None and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
+    if out is None and torch.is_grad_enabled() and (
+            q.requires_grad or (k is not None and k.requires_grad) or (q_weight is not None and q_weight.requires_grad) or
+            (k_weight is not None and k_weight.requires_grad)):
         how = dict(dims=dims, theta=theta, norm=norm, eps=eps, pairs=pairs, origin=origin, step=step, n_text=n_text, first_token=first_token, stream=stream)
         return _NormRope.apply(q, k, q_weight, k_weight, grid, out_dtype, how)
     two = k is not None
     if two and (k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype):
         raise ValueError("q and k must share shape, strides and type")
     if out is None:
-        with _memory_of(stream):
-            q_out = _new_like(q, out_dtype)
-            k_out = _new_like(k, out_dtype) if two else None
-        _used_here(stream, q_out, k_out)
+        if stream is None:
+            q_out, k_out = _new_outputs(q, out_dtype, two)
+        else:
+            with _memory_of(stream):
+                q_out, k_out = _new_outputs(q, out_dtype, two)
+            _used_here(stream, q_out, k_out)
     else:
         q_out, k_out = out
         if q_out.shape != q.shape or (k_out is not None) != two or (out_dtype is not None and q_out.dtype != out_dtype):
@@ -703,8 +721,7 @@ def psa_select_blocks(q: torch.Tensor, k: torch.Tensor, grid: Sequence[int], til
         raise ValueError("row_ptr (heads * blocks + 1 entries) and col_idx must be contiguous int32 tensors")
     row_ptr, col_idx = out
     if scratch is None:
-        with _memory_of(stream):
-            scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        scratch = _new_scratch(need, q, stream)
     elif scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
         raise ValueError("scratch too small")
     _check(lib().psa_select_blocks(q.data_ptr(), k.data_ptr(), prob, T, H, W, struct.pack("%di" % nh, *each), 1 if keep_self else 0, row_ptr.data_ptr(),
@@ -747,8 +764,7 @@ def psa_attn_fwd_lists(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_pt
     prob = _problem(nh, tile, scale, st[0], st[1], d)
     need = _scratch_bytes("lists", nh, grid, tile, n_text)
     if scratch is None:
-        with _memory_of(stream):
-            scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        scratch = _new_scratch(need, q, stream)
     elif scratch.numel() * scratch.element_size() < need or not scratch.is_contiguous():
         raise ValueError("scratch too small")
     _check(lib().psa_attn_fwd_lists(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), row_ptr.data_ptr(), col_idx.data_ptr(),

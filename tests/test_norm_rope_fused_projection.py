@@ -27,13 +27,13 @@ def test_new_tensors_have_the_strides_of_what_they_are_like():
     for x in (torch.empty((3, 5, 128)), torch.empty((5, 3, 128)).transpose(0, 1), torch.empty((3, 5, 136))[..., :128], fused, fused[:, :1], fused[0],
               torch.empty((3, 0, 128)), torch.empty((1, 1, 128)).as_strided((1, 1, 128), (7, 9, 1))):
         for dtype in (None, torch.bfloat16):
-            y = B._new_like(x, dtype)
-            assert y.shape == x.shape and y.stride() == x.stride() and y.dtype == (dtype or x.dtype)
+            for y in B._new_outputs(x, dtype, True):
+                assert y.shape == x.shape and y.stride() == x.stride() and y.dtype == (dtype or x.dtype)
     # elements that share memory: heads half a row apart, tokens half a row apart
     for strides in ((64, 512, 1), (1024, 64, 1), (128, 128, 1)):
         x = torch.empty(8192).as_strided((2, 5, 128), strides)
-        y = B._new_like(x)
-        assert y.shape == x.shape and len(set((y.stride(0) * a + y.stride(1) * b) for a in range(2) for b in range(5))) == 10
+        y, none = B._new_outputs(x, None, False)
+        assert none is None and y.shape == x.shape and len(set((y.stride(0) * a + y.stride(1) * b) for a in range(2) for b in range(5))) == 10
         assert sorted(y.stride()) in ([1, 128, 256], [1, 128, 640])
 
 
