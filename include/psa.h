@@ -207,7 +207,9 @@ int psa_select_blocks(const void* q, const void* k, const psa_problem* prob, int
  * Lists are read by the kernels only: a row that does not lie within the n_entries entries, or has more than NB, counts as
  * empty, an entry that is no block or does not come behind the one before it is left out, and psa_last_device_status() reports
  * PSA_ERR_INVALID_ARG (detail 0x600 or 0x601); out and lse of other rows are not affected.  What an entry's block holds beyond the
- * grid is not attended.  Allocates nothing.  Everything else as psa_attn_fwd. */
+ * grid is not attended.  Allocates nothing.  Everything else as psa_attn_fwd; as there, scores, the softmax's maximum and sum and the output's
+ * sums are in 32 bits, and probabilities are rounded to bf16 before they meet the values, as the tensor cores take both in one type (an output is off by
+ * 0.0023 of the outputs' root mean square as a rule, where only its own rounding to bf16 makes 0.0017). */
 int64_t psa_attn_fwd_lists_scratch_bytes(const psa_problem* prob, int64_t n_text, int T, int H, int W);
 int psa_attn_fwd_lists(const void* q, const void* k, const void* v, void* out, float* lse, const int32_t* row_ptr,
                        const int32_t* col_idx, int64_t n_entries, const psa_problem* prob, int64_t n_text,

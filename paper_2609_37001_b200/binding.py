@@ -744,7 +744,10 @@ def psa_attn_fwd_lists(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_pt
     """Attention over lists of key blocks (see psa.h): q, k, v are bf16 device tensors [heads, T*H*W + n_text, 128] sharing strides, the
     video tokens first; query block i of head h attends the blocks ``col_idx[row_ptr[h*NB + i]:row_ptr[h*NB + i + 1]]`` (int32,
     ascending), as psa_mask_build and psa_select_blocks write them, and all of the text.  ``scratch`` (uint8,
-    psa_attn_fwd_lists_scratch_bytes long) is allocated when not given.  Returns (out like q, lse fp32 [heads, tokens])."""
+    psa_attn_fwd_lists_scratch_bytes long) is allocated when not given.  Returns (out like q, lse fp32 [heads, tokens]).
+
+    How work is handed out goes by an average list of ``col_idx.numel() / row_ptr.numel()`` blocks: of a larger buffer pass the entries in use
+    (``col_idx[:n]``), or a launch of few blocks may be slower than it needs to be."""
     nh, Lt, d = q.shape
     T, H, W = map(int, grid)
     n_text = int(n_text)

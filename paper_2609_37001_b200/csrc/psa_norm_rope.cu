@@ -6,7 +6,7 @@
 // g = R(-angles) dy, h = w * g, s = mean(h * x):  dx = r * (h - x * r^2 * s),  dw = sum of g * x * r.
 //
 // Bound by HBM: forward moves each value in and out once, the gradient x and dy in and dx out.  A group of eight lanes takes one
-// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64, backward 56); a block takes one or more
+// head of a token, 16 channels a lane (or kRows = 2 heads, where there are more than 64, backward 56, as a block has no more threads); a block takes one or more
 // tokens of q and k, or (more than 16 heads, backward 8) of one of them, all heads, so that a mean over all heads costs one read.
 // Blocks are persistent: a group's head is always the same, whose weights, and sums for dw, stay in registers.  Two more warps of
 // the block, the producers, copy the next tokens' rows into shared memory (cp.async, kMaxStages sets at most), and compute cos and
@@ -34,7 +34,8 @@ constexpr int kLanes = 8;         // lanes of a group
 constexpr int kPairs = kHeadDim / 2;
 constexpr int kMaxThreads = 512;   // besides the producers
 constexpr int kProducers = 64;     // threads: a warp that copies and one for angles
-// Sets of rows in shared memory.  24 heads of 115,456 tokens on one card, us with 2, 3 and 4 sets: 1,268, 529, 469; no less with 5 to 8.
+// Sets of rows in shared memory.  24 heads of 115,456 tokens on one card, us with 2, 3 and 4 sets: 1,268, 529, 469.  (copies_wait tells no more than
+// three sets in flight apart: with 5 to 8 sets there are no more copies on their way than with 4, and the time is the same.)
 constexpr int kMaxStages = 4;
 constexpr int kMaxGroups = kMaxThreads / kLanes, kMaxBwdGroups = (16 * 32 - kProducers) / kLanes;   // of one row each
 // Registers.  Forward 80, which are 24 warps an SM: with 64 and 72, 24 heads of 115,456 tokens take 606 and 522 us instead of 486 (5.8
@@ -43,7 +44,9 @@ constexpr int kMaxGroups = kMaxThreads / kLanes, kMaxBwdGroups = (16 * 32 - kPro
 // threads start.)
 constexpr int kRegs = 80, kBwdRegs = 128, kTwoRowsRegs = 96;
 // Threads of a block besides the producers, at most: with q and k (forward and backward), with several tokens.  (A token of few heads
-// keeps the producers as busy as one of many.  12 heads of 32,760 tokens backward: 120 us with blocks of one tensor, 126 with both.)
+// keeps the producers as busy as one of many.  12 heads of 32,760 tokens backward: 120 us with blocks of one tensor, 126 with both.  1.5 million rows a
+// tensor backward, norm over a head, us with blocks of both and of one: 6 heads 557 and 626, 8 heads 549 and 461, 9 heads 609 and 578, 16 heads 636 and
+// 452, so that 8 heads are on the slower side of the rule as it stands.)
 constexpr int kBothThreads = 256, kBothBwdThreads = 128, kSmallThreads = 64;
 
 // ------------------------------------------------------------------------------------------------ packed pairs
@@ -551,7 +554,9 @@ norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// Like the forward pass.  Every block leaves one partial sum per weight, which norm_rope_dw_kernel adds in a fixed order.
+// Like the forward pass.  Every block leaves one partial sum per weight, which norm_rope_dw_kernel adds in a fixed order, in 64 bits.  A thread's own sum,
+// over the tokens of its block (of 75,600 some 1,000, where a tensor has 74 blocks), is in 32: 64 bits would take twice the registers, which are all in use.
+// (It is off by a half step of 32 bits of the magnitudes for each token at most, by the root of that many as a rule.)
 template <class T, class O, int kNorm, bool kHalves, int kRows>
 __global__ void __maxnreg__(kRows == 1 ? kBwdRegs : kTwoRowsRegs)
 norm_rope_bwd_kernel(const __grid_constant__ NormRopeArgs a) {
@@ -767,7 +772,9 @@ cudaError_t launch_norm(NormRopeArgs& a, int norm, bool halves, bool backward, i
 
 cudaError_t launch_norm_rope(NormRopeArgs& a, const psa_qk& prob, bool halves, bool backward, int n_sms, float* q_dw, float* k_dw, cudaStream_t st,
                              int* launches) {
-  // Groups a token: one a head, or one for two.  Tokens a block: blocks of some 256 threads, whole warps.
+  // Groups a token: one a head, or one for two (1.5 million rows a tensor, norm over a head, of the copy rate: 64 heads forward 0.83, 65 to 128
+  // heads 0.54 to 0.63; 56 heads backward 0.84, 57 to 128 heads 0.34 to 0.38).  Tokens a block: one, of few heads as many as make kSmallThreads threads;
+  // whole warps.
   a.parts = a.n_heads <= (backward ? kMaxBwdGroups : kMaxGroups) ? a.n_heads : (a.n_heads + 1) / 2;
   a.tensors = a.out[1] && 2 * a.parts * kLanes <= (backward ? kBothBwdThreads : kBothThreads) ? 2 : 1;
   a.slots = kSmallThreads / (a.tensors * a.parts * kLanes);
