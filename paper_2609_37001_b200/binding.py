@@ -4,6 +4,9 @@ Every step of the path runs inside the CUDA library; torch is used for device me
 and streams.  Importing this module without a built library, or calling it without a
 CUDA device, raises -- there is no CPU fallback.  Attention is forward only: its outputs carry no
 gradient.  Norm and rotation (psa_qk_norm_rope) have one.
+
+With ``stream=`` a call runs there instead of on the current stream: its inputs have to be ready there, and what it
+returns is memory of that stream, which the current one may use once it waits for it, and drop while it still does.
 """
 from __future__ import annotations
 
